@@ -3,7 +3,8 @@
  *
  * The library implements the three stages of AnchorAttention's sparse causal
  * prefill attention (arXiv 2505.23520, Section 3; Algorithms 1-3) as hand-written
- * HIP kernels, one GPU, plus a dense causal flash kernel used as comparator.
+ * HIP kernels, one GPU, plus a dense causal flash kernel used as comparator, and the
+ * paged key / value cache that decoding after a prefill reads (kv_append, kv_attn, kv_read).
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -220,6 +221,91 @@ int anchor_attention_prefill(const aa_params *params, const void *q, const void 
  */
 int dense_causal_flash(const aa_params *params, const void *q, const void *k, const void *v,
                        void *out, float *lse, void *stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Paged key / value cache: what follows a prefill
+ * ---------------------------------------------------------------------------------------------
+ * kv_append rotates new queries and keys by their position and writes keys and values into the pages, kv_attn attends from new
+ * queries to everything that is cached of their sequence, kv_read copies cached rows out.  The conventions at the top of this file
+ * hold (device pointers, host params, no allocation, no synchronisation, no state; errors before anything is enqueued).
+ *
+ *  Pages.  Token j of sequence b lies in page  page_table[b*table_stride + j / page_size], row j % page_size.  Pages outside
+ *  [0, n_pages) (-1: not there, released) and tokens at or beyond max_pages*page_size have no storage: nothing is written for them,
+ *  nothing is attended, and kv_read gives zeros.  Sequences may share pages that nobody appends to.
+ *
+ *  New tokens.  kv_len[b] counts the tokens of sequence b INCLUDING the call's n_b new ones: new token i is token
+ *  j = kv_len[b] - n_b + i of the sequence.  Fixed length: n_b = N, row (b, i).  Packed (cu_seqlens != NULL): n_b =
+ *  cu_seqlens[b+1] - cu_seqlens[b] <= N, row cu_seqlens[b] + i; rows at and behind cu_seqlens[B], up to total_tokens (the rows of the
+ *  packed axis), belong to nobody: they are not read, and not written.  j < 0 (more new tokens than the sequence has: left
+ *  padding): the token has no storage and sees no key.
+ *
+ *  Cache formats.  AA_KV_PLAIN: element (page, head, row, c) of the call's dtype at page*kc_stride[0] + head*kc_stride[1] +
+ *  row*kc_stride[2] + c; strides in elements, multiples of 16 bytes.
+ *  AA_KV_FP4: 4-bit floats (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), d/2 bytes a row at
+ *  page*kc_stride[0] + head*kc_stride[1] + row*kc_stride[2] (bytes, multiples of 16), channel 2i in the low and 2i+1 in the high half
+ *  of byte i; and a scale byte for every 32 channels g of a row at  page*ks_stride[0] + head*ks_stride[1] + g*ks_stride[2] + row
+ *  (bytes, multiples of 16).  A value is  code * 2^(byte - 127); byte 255: the group held a NaN or an infinity, its values are NaN.
+ *  kv_append takes the least exponent in [-120, 125] with  max |x| <= 7 * 2^e  over the group's rotated, unrounded values, and the
+ *  nearest code, ties to the even one.  Other bytes that kv_attn and kv_read accept: 7 .. 252.  dtype AA_BF16 only.
+ *  The same for values with vc_stride / vs_stride.
+ */
+enum { AA_KV_PLAIN = 0, AA_KV_FP4 = 1 };
+
+typedef struct aa_kv_params {
+    int32_t B, Hq, Hkv;       /* sequences, query heads, KV heads (Hq % Hkv == 0; each <= 65535)  */
+    int32_t N;                /* new tokens of a sequence; the most of any when cu_seqlens != NULL */
+    int32_t d;                /* head dimension: bf16 -> 64 or 128; fp32 -> 32, 64 or 128           */
+    int32_t dtype;            /* AA_FP32 or AA_BF16: new tokens, outputs and plain pages            */
+    int32_t format;           /* AA_KV_PLAIN or AA_KV_FP4                                           */
+    int32_t page_size;        /* tokens of a page: a power of two, 16 .. 2^20                       */
+    int32_t n_pages;          /* pages of the pool                                                  */
+    int32_t max_pages;        /* entries of a sequence's row of page_table                          */
+    int32_t max_len;          /* kv_attn: longest kv_len, if known; 0: max_pages * page_size.  Chooses */
+                              /* how the keys are dealt to work-groups, and the workspace; a longer   */
+                              /* sequence is still attended whole                                   */
+    int32_t causal;           /* kv_attn: 1: new token i sees tokens 0 .. j; 0: all kv_len[b]           */
+    int32_t rot_dim;          /* kv_append: channels 0 .. rot_dim-1 are rotated; a multiple of 16, 0: none */
+    int32_t rot_interleaved;  /* 0: pairs (i, i + rot_dim/2); 1: pairs (2i, 2i + 1)                 */
+    float   softmax_scale;    /* kv_attn: 0 -> 1/sqrt(d)                                           */
+    int64_t q_stride[3], k_stride[3], v_stride[3]; /* batch, head, token; elements, as in aa_params */
+    int64_t o_stride[3];      /* kv_attn: out; kv_append: q_out                                    */
+    int64_t ko_stride[3];     /* kv_append: k_out                                                  */
+    void *kc, *vc;            /* pools of pages                                                    */
+    int64_t kc_stride[3], vc_stride[3];            /* page, head, row                             */
+    uint8_t *ks, *vs;         /* AA_KV_FP4: scale bytes                                            */
+    int64_t ks_stride[3], vs_stride[3];            /* page, head, group of 32 channels            */
+    const int32_t *page_table;/* device int32[B][table_stride]                                     */
+    int64_t table_stride;
+    const int32_t *kv_len;    /* device int32[B]                                                   */
+    const int32_t *cu_seqlens;/* device int32[B+1] or NULL                                         */
+    int64_t total_tokens;     /* rows of the packed axis; ignored when cu_seqlens == NULL          */
+} aa_kv_params;
+
+/*
+ * For every new token: pos = positions[row] (device int32 per row b*N + i or packed row), or j where positions is NULL.  Channel
+ * pair i of every query and key head is turned by  t = pos * inv_freq[i]  (inv_freq: device float[rot_dim/2], t in 64 bits):
+ *   y1 = x1 cos t - x2 sin t,   y2 = x2 cos t + x1 sin t.
+ * Writes the turned keys and the values into the pages, the turned queries to q_out and the turned keys to k_out (each may be NULL;
+ * q and q_out together; q_out == q and k_out == k with equal strides: in place).  k and v may both be NULL: queries only.
+ * inv_freq may be NULL where rot_dim is 0.  Two new tokens must not have the same storage.
+ */
+int kv_append(const aa_kv_params *params, const void *q, const void *k, const void *v, const float *inv_freq,
+              const int32_t *positions, void *q_out, void *k_out, void *stream);
+
+/* *bytes_out = workspace of kv_attn (0 where it needs none).  Host only. */
+int kv_attn_workspace_bytes(const aa_kv_params *params, size_t *bytes_out);
+
+/*
+ * out_r = sum_j softmax_j(softmax_scale * <q_r, k_j>) v_j over the cached tokens that row r sees, lse_r = log sum_j exp(...)
+ * (lse nullable, laid out as the per-row arrays at the top).  A row that sees no key: out 0, lse -infinity.  What lies in
+ * storage that no row of a sequence sees (behind its end, other pages) never reaches an output, whatever its bits; a value row that
+ * is not finite reaches every row of its sequence that it is computed with.
+ */
+int kv_attn(const aa_kv_params *params, const void *q, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* k_out, v_out (k_stride, v_stride; either may be NULL): the rows of every sequence's new tokens as the cache holds them. */
+int kv_read(const aa_kv_params *params, void *k_out, void *v_out, void *stream);
 
 const char *anchor_strerror(int code);
 /* Text of the last HIP error this thread's calls ran into ("" if none). */

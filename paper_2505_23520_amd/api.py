@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libanchor_attention.so")
 
 AA_FP32, AA_BF16 = 0, 1
 AA_STRIPE, AA_BLOCK = 0, 1
+AA_KV_PLAIN, AA_KV_FP4 = 0, 1
 AA_ENGINE_AUTO, AA_ENGINE_128, AA_ENGINE_256 = 0, 1, 2
 AA_OK, AA_EINVAL, AA_EUNSUPPORTED, AA_EWORKSPACE, AA_EHIP = 0, -1, -2, -3, -4
 
@@ -47,8 +48,27 @@ class aa_sizes(ctypes.Structure):
     ]
 
 
+class aa_kv_params(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("N", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("format", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("max_len", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32), ("rot_interleaved", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("o_stride", ctypes.c_int64 * 3), ("ko_stride", ctypes.c_int64 * 3),
+        ("kc", ctypes.c_void_p), ("vc", ctypes.c_void_p),
+        ("kc_stride", ctypes.c_int64 * 3), ("vc_stride", ctypes.c_int64 * 3),
+        ("ks", ctypes.c_void_p), ("vs", ctypes.c_void_p),
+        ("ks_stride", ctypes.c_int64 * 3), ("vs_stride", ctypes.c_int64 * 3),
+        ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("kv_len", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p), ("total_tokens", ctypes.c_int64),
+    ]
+
+
 _P = ctypes.c_void_p
 _PP = ctypes.POINTER(aa_params)
+_PK = ctypes.POINTER(aa_kv_params)
 _SIGNATURES = {
     "anchor_sizes": (ctypes.c_int, [_PP, ctypes.POINTER(aa_sizes)]),
     "anchor_workspace_bytes": (ctypes.c_int, [_PP, ctypes.POINTER(ctypes.c_size_t)]),
@@ -58,6 +78,10 @@ _SIGNATURES = {
     "sparse_attn": (ctypes.c_int, [_PP, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_int64, _P, _P, _P]),
     "anchor_attention_prefill": (ctypes.c_int, [_PP, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "dense_causal_flash": (ctypes.c_int, [_PP, _P, _P, _P, _P, _P, _P]),
+    "kv_append": (ctypes.c_int, [_PK, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "kv_attn_workspace_bytes": (ctypes.c_int, [_PK, ctypes.POINTER(ctypes.c_size_t)]),
+    "kv_attn": (ctypes.c_int, [_PK, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "kv_read": (ctypes.c_int, [_PK, _P, _P, _P]),
     "anchor_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "anchor_last_hip_error": (ctypes.c_char_p, []),
 }
@@ -221,6 +245,154 @@ def alloc_stage_buffers(p: aa_params, device="cuda", want_acc=True, idx_capacity
         ws=torch.empty(max(s.select_ws_bytes, 256), dtype=torch.uint8, device=device),
         lse=torch.empty(s.rows, **f32),
     )
+
+
+# ------------------------------------------------------------------ paged key / value cache
+def alloc_kv_cache(n_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16, format=AA_KV_PLAIN, device="cuda") -> dict:
+    """Pools for n_pages pages: k, v [n_pages, Hkv, page_size, d] of dtype, or for AA_KV_FP4 their codes uint8 [.., d // 2] and
+    k_scale, v_scale uint8 [n_pages, Hkv, d // 32, page_size].  Cleared, though no kernel lets what is behind a sequence's end
+    reach an output."""
+    if format == AA_KV_PLAIN:
+        k, v = (torch.zeros(n_pages, Hkv, page_size, d, dtype=dtype, device=device) for _ in range(2))
+        return dict(k=k, v=v, k_scale=None, v_scale=None)
+    u8 = dict(dtype=torch.uint8, device=device)
+    k, v = (torch.zeros(n_pages, Hkv, page_size, d // 2, **u8) for _ in range(2))
+    ks, vs = (torch.full((n_pages, Hkv, d // 32, page_size), 127, **u8) for _ in range(2))
+    return dict(k=k, v=v, k_scale=ks, v_scale=vs)
+
+
+def _kv_strides(t, packed):
+    """Strides of a tensor of new tokens; a dimension of one entry has none that matters."""
+    if t.dim() != (3 if packed else 4):
+        raise ValueError("new tokens are [B, H, n, d], or [H, total, d] with cu_seqlens: got shape %s" % (tuple(t.shape),))
+    if t.stride(-1) != 1:
+        raise ValueError("the last dimension has to be contiguous: strides %s" % (t.stride(),))
+    s = [0 if n == 1 else st for n, st in zip(t.shape[:-1], t.stride()[:-1])]
+    return (ctypes.c_int64 * 3)(*(([0] if packed else []) + s))
+
+
+def _pool_strides(t, unit):
+    """Strides of a pool (rows of `unit` entries); for a dimension of one entry any multiple of a row."""
+    s, step = [], unit
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        s.append(step if n == 1 else st)
+        step = max(step, s[-1] * n)
+    return (ctypes.c_int64 * 3)(*reversed(s))
+
+
+def make_kv_params(cache: dict, page_table, kv_len, q=None, k=None, v=None, out=None, k_out=None, cu_seqlens=None, max_new=None,
+                   max_len: int = 0, causal: bool = True, rot_dim: int = 0, rot_interleaved: bool = False,
+                   softmax_scale: float = 0.0, Hq=None) -> aa_kv_params:
+    """Describe one call on the paged cache `cache` (alloc_kv_cache, or pools of any strides with whole rows).
+
+    page_table int32 [B, max_pages], kv_len int32 [B] (tokens of each sequence, the new ones included).  New tokens: q [B, Hq, n, d],
+    k, v [B, Hkv, n, d], or with cu_seqlens (device int32 [B + 1]) packed [Hq, total, d] and [Hkv, total, d], max_new the most of any
+    sequence.  kv_append: q, k, v, out (the turned queries), k_out (the turned keys).  kv_attn: q, out.  kv_read: k, v (where it
+    writes).  The tensors named here are kept alive by the result; calls take tensors of the same strides."""
+    named = dict(q=q, k=k, v=v, out=out, k_out=k_out)
+    given = {n: t for n, t in named.items() if t is not None}
+    if not given:
+        raise ValueError("no tensor of new tokens: name the ones that the call takes")
+    first, packed = next(iter(given.values())), cu_seqlens is not None
+    p = aa_kv_params()
+    p.format = AA_KV_PLAIN if cache.get("k_scale") is None else AA_KV_FP4
+    p.dtype = _kv_dtype(first)
+    p.n_pages, p.Hkv, p.page_size = cache["k"].shape[:3]
+    p.d = first.shape[-1]
+    heads = q if q is not None else out
+    p.Hq = heads.shape[-3] if heads is not None else int(Hq or p.Hkv)
+    p.B, p.max_pages = page_table.shape
+    axis = first.shape[-2]
+    p.N = int(axis if max_new is None else max_new)
+    for name, t in given.items():
+        want = (p.Hq if name in ("q", "out") else p.Hkv, axis, p.d)
+        if tuple(t.shape) != (want if packed else (p.B,) + want) or t.dtype != first.dtype:
+            raise ValueError("%s: shape %s %s, expected %s %s" % (name, tuple(t.shape), t.dtype,
+                                                                want if packed else (p.B,) + want, first.dtype))
+    if not packed and p.N != axis:
+        raise ValueError("max_new %d of a batch with %d new tokens a sequence" % (p.N, axis))
+    if p.format == AA_KV_PLAIN:
+        shapes = dict(k=((p.n_pages, p.Hkv, p.page_size, p.d), first.dtype))
+    else:
+        shapes = dict(k=((p.n_pages, p.Hkv, p.page_size, p.d // 2), torch.uint8),
+                      k_scale=((p.n_pages, p.Hkv, p.d // 32, p.page_size), torch.uint8))
+    for key, (shape, dtype) in shapes.items():
+        for t in (cache[key], cache[key.replace("k", "v", 1)]):
+            if tuple(t.shape) != shape or t.dtype != dtype or t.stride(-1) != 1:
+                raise ValueError("cache[%r]: shape %s %s, expected %s %s with contiguous rows" % (key, tuple(t.shape), t.dtype, shape, dtype))
+    ints = [("page_table", page_table, (p.B, p.max_pages)), ("kv_len", kv_len, (p.B,))]
+    if packed:
+        ints.append(("cu_seqlens", cu_seqlens, (p.B + 1,)))
+    for name, t, shape in ints:
+        if t.dtype != torch.int32 or tuple(t.shape) != shape or t.stride(-1) != 1:
+            raise ValueError("%s: shape %s %s, expected contiguous int32 %s" % (name, tuple(t.shape), t.dtype, shape))
+    held = list(given.values()) + [t for t in cache.values() if t is not None] + [page_table, kv_len] + ([cu_seqlens] if packed else [])
+    if any(t.device != first.device for t in held):
+        raise ValueError("tensors on different devices: %s" % sorted({str(t.device) for t in held}))
+    for field, t in (("q_stride", q), ("k_stride", k), ("v_stride", v), ("o_stride", out), ("ko_stride", k_out)):
+        if t is not None:
+            setattr(p, field, _kv_strides(t, packed))
+    p.kc, p.vc = cache["k"].data_ptr(), cache["v"].data_ptr()
+    p.kc_stride, p.vc_stride = (_pool_strides(cache[x], cache[x].shape[-1]) for x in ("k", "v"))
+    if p.format == AA_KV_FP4:
+        p.ks, p.vs = cache["k_scale"].data_ptr(), cache["v_scale"].data_ptr()
+        p.ks_stride, p.vs_stride = (_pool_strides(cache[x], p.page_size) for x in ("k_scale", "v_scale"))
+    p.page_table, p.kv_len = page_table.data_ptr(), kv_len.data_ptr()
+    p.table_stride = p.max_pages if p.B == 1 else page_table.stride(0)
+    p.cu_seqlens = cu_seqlens.data_ptr() if packed else None
+    p.total_tokens = axis if packed else 0
+    p.max_len, p.causal = int(max_len), int(bool(causal))
+    p.rot_dim, p.rot_interleaved, p.softmax_scale = int(rot_dim), int(bool(rot_interleaved)), softmax_scale
+    p.device = first.device
+    p.held = held
+    return p
+
+
+def _kv_dtype(t):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("new tokens are float32 or bfloat16: got %s" % t.dtype)
+    return AA_FP32 if t.dtype == torch.float32 else AA_BF16
+
+
+def _kv_call(fn, p, tensors, strides, args, stream):
+    """Calls fn on the device of p's tensors; tensors are checked against what p was made for."""
+    for t, field in zip(tensors, strides):
+        if t is not None and (t.device != p.device or field and tuple(_kv_strides(t, bool(p.cu_seqlens))) != tuple(getattr(p, field))):
+            raise ValueError("a tensor on %s with strides %s, where the params were made for %s%s"
+                             % (t.device, t.stride(), p.device, " and " + str(tuple(getattr(p, field))) if field else ""))
+    with torch.cuda.device(p.device):
+        _check(fn(ctypes.byref(p), *args, _stream(stream)))
+
+
+def kv_attn_workspace_bytes(p: aa_kv_params) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.kv_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(n)))
+    return int(n.value)
+
+
+def kv_append(p, q, k, v, inv_freq=None, positions=None, q_out=None, k_out=None, stream=None):
+    """Turn the new queries and keys by their position (q_out, k_out) and store keys and values in the cache's pages.
+    inv_freq float32 [rot_dim // 2]; positions int32, one a new token ([B, n] or packed), None: its place in the sequence."""
+    if p.rot_dim and (inv_freq is None or inv_freq.dtype != torch.float32 or inv_freq.numel() != p.rot_dim // 2 or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq: contiguous float32 [%d] expected" % (p.rot_dim // 2))
+    if positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous()
+                                  or positions.numel() != (p.total_tokens if p.cu_seqlens else p.B * p.N)):
+        raise ValueError("positions: contiguous int32, one a new token, expected")
+    _kv_call(_lib.kv_append, p, (q, k, v, q_out, k_out, inv_freq, positions),
+             ("q_stride", "k_stride", "v_stride", "o_stride", "ko_stride", None, None),
+             (_ptr(q), _ptr(k), _ptr(v), _ptr(inv_freq), _ptr(positions), _ptr(q_out), _ptr(k_out)), stream)
+
+
+def kv_attn(p, q, out, lse=None, ws=None, stream=None):
+    """Attention of the new queries over the cached tokens that they see; ws: kv_attn_workspace_bytes(p) bytes, of this call alone
+    while it runs."""
+    _kv_call(_lib.kv_attn, p, (q, out, lse, ws), ("q_stride", "o_stride", None, None),
+             (_ptr(q), _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()), stream)
+
+
+def kv_read(p, k_out=None, v_out=None, stream=None):
+    """Copy the rows of every sequence's new tokens out of the cache (4 bits: their values)."""
+    _kv_call(_lib.kv_read, p, (k_out, v_out), ("k_stride", "v_stride"), (_ptr(k_out), _ptr(v_out)), stream)
 
 
 def default_scale(d: int) -> float:

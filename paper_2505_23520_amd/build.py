@@ -13,6 +13,7 @@ LIB = os.path.join(HERE, "libanchor_attention.so")
 PROBE_LIB = os.path.join(HERE, "libanchor_probe.so")
 PROBE_SOURCE = os.path.join("probe", "mfma_probe.hip")
 SOURCES = ["aa_api.hip", "aa_engine_bf16.hip", "aa_engine_bf16_pp.hip", "aa_engine_fp32.hip", "aa_select.hip"]
+CACHE_SOURCES = ["aa_kv_api.hip", "aa_kv_append.hip", "aa_kv_attn.hip"]      # the paged key / value cache
 # The bf16 engines never produce a NaN that is used (masked scores are -inf, the guards around
 # exp(-inf - -inf) select the other arm), so their row-max chains may drop NaN canonicalisation.
 EXTRA = {"aa_engine_bf16.hip": ["-fno-honor-nans"], "aa_engine_bf16_pp.hip": ["-fno-honor-nans"]}
@@ -36,7 +37,7 @@ def build(verbose: bool = False) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=6) as ex:
-        objs = list(ex.map(compile_one, SOURCES + [PROBE_SOURCE]))
+        objs = list(ex.map(compile_one, SOURCES + CACHE_SOURCES + [PROBE_SOURCE]))
     for lib, parts in ((LIB, objs[:-1]), (PROBE_LIB, objs[-1:])):
         r = subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", lib, *parts],
                            capture_output=True, text=True)

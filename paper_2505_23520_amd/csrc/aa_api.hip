@@ -15,13 +15,15 @@
 
 namespace aa {
 namespace {
-
 thread_local char g_hip_err[256] = "";
+}
 
 int hip_fail(hipError_t e, const char* what) {
     snprintf(g_hip_err, sizeof(g_hip_err), "%s: %s", what, hipGetErrorString(e));
     return AA_EHIP;
 }
+
+namespace {
 #define AA_HIP(call)                                         \
     do {                                                     \
         hipError_t e_ = (call);                              \

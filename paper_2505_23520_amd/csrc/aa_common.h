@@ -22,6 +22,9 @@ inline hipError_t launch_kernel(void (*kern)(KArgs...), dim3 grid, dim3 block, s
     return hipLaunchKernel((const void*)kern, grid, block, ptrs, lds, st);
 }
 
+// Keeps the text that anchor_last_hip_error() returns; AA_EHIP.
+int hip_fail(hipError_t e, const char* what);
+
 // Kernel-side copy of the call's parameters (plain data, passed by value).
 struct KParams {
     int B, Hq, Hkv, N, d;

@@ -1,0 +1,152 @@
+"""Host-only checks of the paged cache: argument checks of the C entry points and of the binding, struct layout, the 4-bit format's
+code compiled for the host against the definition."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2505_23520_amd import api as _api
+    return _api
+
+
+def _three(a, b, c):
+    return (ctypes.c_int64 * 3)(a, b, c)
+
+
+def _params(api, **kw):
+    p = api.aa_kv_params()
+    p.B, p.Hq, p.Hkv, p.N, p.d, p.dtype, p.format = 2, 8, 2, 1, 128, api.AA_BF16, api.AA_KV_PLAIN
+    p.page_size, p.n_pages, p.max_pages, p.table_stride, p.causal, p.rot_dim = 16, 10, 4, 4, 1, 128
+    for f in ("q_stride", "o_stride"):
+        setattr(p, f, _three(8 * 128, 128, 128))
+    for f in ("k_stride", "v_stride", "ko_stride"):
+        setattr(p, f, _three(2 * 128, 128, 128))
+    for f in ("kc_stride", "vc_stride"):
+        setattr(p, f, _three(2 * 16 * 128, 16 * 128, 128))
+    for f in ("ks_stride", "vs_stride"):
+        setattr(p, f, _three(2 * 4 * 16, 4 * 16, 16))
+    p.kc = p.vc = p.ks = p.vs = p.page_table = p.kv_len = 4096        # never dereferenced on the host
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+def test_struct_layout(api, tmp_path):
+    """aa_kv_params of the binding is the header's, field by field; the header stays plain C99."""
+    src, exe = tmp_path / "h.c", str(tmp_path / "h")
+    names = [f[0] for f in api.aa_kv_params._fields_]
+    src.write_text('#include "anchor_attention.h"\n#include <stdio.h>\nint main(void) {\nprintf("%zu\\n", sizeof(aa_kv_params));\n'
+                   + "".join('printf("%%zu\\n", offsetof(aa_kv_params, %s));\n' % n for n in names) + "return 0; }\n")
+    subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Wextra", "-pedantic", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", exe])
+    got = [int(x) for x in subprocess.check_output([exe], text=True).split()]
+    assert got == [ctypes.sizeof(api.aa_kv_params)] + [getattr(api.aa_kv_params, n).offset for n in names]
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), -1), (dict(Hq=7), -1), (dict(Hkv=0), -1), (dict(N=0), -1), (dict(d=0), -1), (dict(dtype=2), -1), (dict(format=2), -1),
+    (dict(page_size=0), -1), (dict(page_size=24), -1), (dict(page_size=-16), -1), (dict(n_pages=0), -1), (dict(max_pages=0), -1),
+    (dict(max_len=-1), -1), (dict(causal=2), -1), (dict(rot_dim=-16), -1), (dict(rot_dim=256), -1), (dict(rot_dim=7), -1),
+    (dict(rot_interleaved=2), -1), (dict(softmax_scale=float("nan")), -1), (dict(softmax_scale=-1.0), -1), (dict(table_stride=3), -1),
+    (dict(page_table=None), -1), (dict(kv_len=None), -1), (dict(cu_seqlens=4096, total_tokens=0), -1),
+    (dict(cu_seqlens=4096, total_tokens=3, N=4), -1), (dict(kc=None), -1), (dict(vc=4100), -1), (dict(format=1, ks=None), -1),
+    (dict(format=1, vs=4104), -1), (dict(kc_stride=_three(4096, 2048, 100)), -1), (dict(vc_stride=_three(4096, 2048, 132)), -1),
+    (dict(kc_stride=_three(-4096, 2048, 128)), -1), (dict(kc_stride=_three(0, 2048, 128)), -1), (dict(vc_stride=_three(1 << 59, 2048, 128)), -1),
+    (dict(format=1, ks_stride=_three(128, 64, 8)), -1), (dict(format=1, ks_stride=_three(128, 72, 16)), -1),
+    (dict(d=96, rot_dim=0), -2), (dict(d=256), -2), (dict(d=32, rot_dim=0), -2), (dict(page_size=8), -2), (dict(page_size=1 << 21), -2), (dict(rot_dim=24), -2),
+    (dict(format=1, dtype=0), -2), (dict(B=65536), -2), (dict(Hq=65536, Hkv=1), -2), (dict(B=65535, N=65535), -2), (dict(N=2**30, B=1), -2),
+])
+def test_rejects_bad_params(api, kw, code):
+    """Before anything is enqueued: no GPU here, and none is asked for."""
+    n = ctypes.c_size_t()
+    p = _params(api, **kw)
+    assert api._lib.kv_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(n)) == code
+    assert api._lib.kv_append(ctypes.byref(p), 4096, 4096, 4096, 4096, None, 4096, None, None) == code
+    assert api._lib.kv_attn(ctypes.byref(p), 4096, 4096, None, 4096, 1 << 40, None) == code
+    assert api._lib.kv_read(ctypes.byref(p), 4096, 4096, None) == code
+
+
+def test_rejects_bad_calls(api):
+    lib, ref = api._lib, ctypes.byref
+    p = _params(api)
+    ok = 4096
+    E = api.AA_EINVAL
+    assert lib.kv_append(None, ok, ok, ok, ok, None, ok, None, None) == E
+    for args in ((None, None, None, ok, None, None, None),       # nothing to do
+                 (ok, ok, ok, ok, None, None, None),             # queries without q_out
+                 (None, ok, ok, ok, None, ok, None),             # q_out without queries
+                 (ok, ok, None, ok, None, ok, None), (ok, None, ok, ok, None, ok, None), (ok, None, None, ok, None, ok, ok),
+                 (ok, ok, ok, None, None, ok, None),             # rotation without frequencies
+                 (ok + 2, ok, ok, ok, None, ok, None), (ok, ok + 8, ok, ok, None, ok, None), (ok, ok, ok, ok, None, ok + 4, None)):
+        assert lib.kv_append(ref(p), *args, None) == E, args
+    for field, st in (("q_stride", (1024, 128, 4)), ("k_stride", (256, -128, 128)), ("v_stride", (1 << 40, 128, 128)), ("o_stride", (0, 128, 128)),
+                      ("o_stride", (1024, 64, 128)), ("ko_stride", (256, 0, 128))):
+        q = _params(api, **{field: _three(*st)})
+        assert lib.kv_append(ref(q), ok, ok, ok, ok, None, ok, ok, None) == E, field
+    q = _params(api, N=3, o_stride=_three(8 * 128, 128, 64))
+    assert lib.kv_attn(ref(q), ok, ok, None, ok, 1 << 40, None) == E                       # rows of out that overlap
+    assert lib.kv_attn(ref(p), None, ok, None, ok, 1 << 40, None) == E
+    assert lib.kv_attn(ref(p), ok, ok + 2, None, ok, 1 << 40, None) == E
+    assert lib.kv_read(ref(p), None, None, None) == E
+    assert lib.kv_attn_workspace_bytes(ref(p), None) == E
+
+
+def test_binding_rejects(api):
+    c = api.alloc_kv_cache(6, 2, 16, 128, device="cpu")
+    c4 = api.alloc_kv_cache(6, 2, 16, 128, format=api.AA_KV_FP4, device="cpu")
+    table, lens = torch.zeros(3, 2, dtype=torch.int32), torch.ones(3, dtype=torch.int32)
+    q, k = torch.zeros(3, 8, 1, 128, dtype=torch.bfloat16), torch.zeros(3, 2, 1, 128, dtype=torch.bfloat16)
+    p = api.make_kv_params(c, table, lens, q=q, k=k, v=k, out=q)
+    assert (p.B, p.Hq, p.Hkv, p.N, p.d, p.page_size, p.max_pages, p.format) == (3, 8, 2, 1, 128, 16, 2, api.AA_KV_PLAIN)
+    assert api.make_kv_params(c4, table, lens, q=q, out=q).format == api.AA_KV_FP4
+    bad = [dict(), dict(q=q[:2]), dict(q=q, out=q.float()), dict(q=q, k=k[:, :1]), dict(q=q.half()), dict(q=q[0]),
+           dict(q=q.transpose(2, 3).contiguous().transpose(2, 3)[..., ::2]), dict(q=q, max_new=2), dict(q=q[..., :64], k=k[..., :64])]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            api.make_kv_params(c, table, lens, **kw)
+    for cache, t, n in ((c, table.long(), lens), (c, table, lens[:2]), (c, table, lens.float()), (dict(c, v=c["v"][:5]), table, lens),
+                        (dict(c, k=c["k"].float()), table, lens), (dict(c4, v_scale=c4["v_scale"][:, :, :2]), table, lens)):
+        with pytest.raises(ValueError):
+            api.make_kv_params(cache, t, n, q=q, out=q)
+    f = torch.ones(64)
+    p = api.make_kv_params(c, table, lens, q=q, k=k, v=k, out=q, rot_dim=128)
+    for args in ((q, k, k, f[:32], None, q), (q, k, k, f.double(), None, q), (q, k, k, None, None, q), (q, k, k, f, torch.zeros(3), q),
+                 (q, k, k, f, torch.zeros(2, dtype=torch.int32), q), (q.expand(3, 8, 1, 128)[:, ::2], k, k, f, None, q)):
+        with pytest.raises(ValueError):
+            api.kv_append(p, *args)
+
+
+def test_fp4_code_on_the_host(tmp_path):
+    """fp4_scale_byte, fp4_code and fp4_value against every code and exponent tried out."""
+    from kv_util import fp4_pack, fp4_values
+    src, exe = tmp_path / "f.cpp", str(tmp_path / "f")
+    src.write_text('''#include "%s/paper_2505_23520_amd/csrc/aa_kv_fp4.h"
+#include <stdio.h>
+#include <string.h>
+int main() {
+    double x[32];
+    while (fread(x, 8, 32, stdin) == 32) {
+        uint64_t top = 0;
+        for (int i = 0; i < 32; ++i) { uint64_t u; memcpy(&u, x + i, 8); u &= 0x7fffffffffffffffull; if (u > top) top = u; }
+        const int byte = aa::fp4_scale_byte(top);
+        for (int i = 0; i < 32; ++i) {
+            const unsigned c = byte == 255 ? 0 : aa::fp4_code(x[i] * aa::fp4_inverse_scale(byte));
+            printf("%%.17g\\n", (double)aa::fp4_value(c, byte));
+        }
+    }
+}''' % ROOT)
+    subprocess.check_call(["g++", "-O2", "-std=c++17", str(src), "-o", exe])
+    gen = torch.Generator().manual_seed(1)
+    x = torch.randn(400, 32, generator=gen, dtype=torch.float64)
+    x = torch.cat([x, (x * 8).round() / 8, (x[:100] * 4).round(), x[:50] * 2.0 ** -125, x[:50] * 2.0 ** 125, torch.zeros(1, 32)])
+    x[3, 4], x[5, 6], x[7, 8] = float("inf"), float("nan"), -float("inf")
+    got = subprocess.run([exe], input=x.numpy().tobytes(), capture_output=True, check=True).stdout.split()
+    got = torch.tensor([float(t) for t in got], dtype=torch.float64).view(-1, 32)
+    want = fp4_values(*fp4_pack(x))
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(), want.nan_to_num())
