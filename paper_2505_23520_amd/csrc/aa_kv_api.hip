@@ -28,6 +28,8 @@ int check_pool(const aa_kv_params* p, const void* pool, const int64_t* st, const
     if (!pool || unaligned(pool)) return AA_EINVAL;
     if (fp4 && (!sc || unaligned(sc))) return AA_EINVAL;
     if (st[0] > (1ll << 60) / p->n_pages || (fp4 && ss[0] > (1ll << 60) / p->n_pages)) return AA_EINVAL;
+    // 16 rows, and the groups of a row, are addressed with 32 bits from the page's first
+    if (st[2] >= (1 << 25) || (fp4 && ss[2] >= (1 << 28))) return AA_EUNSUPPORTED;
     for (int e = 0; e < 3; ++e) {
         if (st[e] < row || st[e] % unit || st[e] >= (1ll << 40)) return AA_EINVAL;
         if (fp4 && (ss[e] < p->page_size || ss[e] % 16 || ss[e] >= (1ll << 40))) return AA_EINVAL;
@@ -52,6 +54,7 @@ int make_args(const aa_kv_params* p, KvArgs* a) {
     if (p->format == AA_KV_FP4 && p->dtype != AA_BF16) return AA_EUNSUPPORTED;
     if (p->page_size < 16 || p->page_size > (1 << 20)) return AA_EUNSUPPORTED;
     if (p->rot_dim % 16) return AA_EUNSUPPORTED;
+    if ((int64_t)p->max_pages * p->page_size > (1 << 30)) return AA_EUNSUPPORTED;       // tokens of a sequence are counted in 32 bits
     // heads and sequences stand on y and z of a launch grid, tokens on x; new rows of a KV head stay below 2^31
     if (p->B > 65535 || p->Hq > 65535) return AA_EUNSUPPORTED;
     const int64_t tokens = p->cu_seqlens ? p->total_tokens : (int64_t)p->B * p->N;
