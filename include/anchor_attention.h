@@ -284,7 +284,7 @@ typedef struct aa_kv_params {
 
 /*
  * For every new token: pos = positions[row] (device int32 per row b*N + i or packed row), or j where positions is NULL.  Channel
- * pair i of every query and key head is turned by  t = pos * inv_freq[i]  (inv_freq: device float[rot_dim/2], t in 64 bits):
+ * pair i of every query and key head is turned by  t = pos * inv_freq[i]  (inv_freq: device float[rot_dim/2]; t in 64 bits, |t| < 2^40):
  *   y1 = x1 cos t - x2 sin t,   y2 = x2 cos t + x1 sin t.
  * Writes the turned keys and the values into the pages, the turned queries to q_out and the turned keys to k_out (each may be NULL;
  * q and q_out together; q_out == q and k_out == k with equal strides: in place).  k and v may both be NULL: queries only.

@@ -261,6 +261,9 @@ def alloc_kv_cache(n_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.b
     return dict(k=k, v=v, k_scale=ks, v_scale=vs)
 
 
+_KV_FIELDS = dict(q="q_stride", k="k_stride", v="v_stride", out="o_stride", k_out="ko_stride")
+
+
 def _kv_strides(t, packed):
     """Strides of a tensor of new tokens; a dimension of one entry has none that matters."""
     if t.dim() != (3 if packed else 4):
@@ -329,9 +332,8 @@ def make_kv_params(cache: dict, page_table, kv_len, q=None, k=None, v=None, out=
     held = list(given.values()) + [t for t in cache.values() if t is not None] + [page_table, kv_len] + ([cu_seqlens] if packed else [])
     if any(t.device != first.device for t in held):
         raise ValueError("tensors on different devices: %s" % sorted({str(t.device) for t in held}))
-    for field, t in (("q_stride", q), ("k_stride", k), ("v_stride", v), ("o_stride", out), ("ko_stride", k_out)):
-        if t is not None:
-            setattr(p, field, _kv_strides(t, packed))
+    for name, t in given.items():
+        setattr(p, _KV_FIELDS[name], _kv_strides(t, packed))
     p.kc, p.vc = cache["k"].data_ptr(), cache["v"].data_ptr()
     p.kc_stride, p.vc_stride = (_pool_strides(cache[x], cache[x].shape[-1]) for x in ("k", "v"))
     if p.format == AA_KV_FP4:
@@ -344,7 +346,9 @@ def make_kv_params(cache: dict, page_table, kv_len, q=None, k=None, v=None, out=
     p.max_len, p.causal = int(max_len), int(bool(causal))
     p.rot_dim, p.rot_interleaved, p.softmax_scale = int(rot_dim), int(bool(rot_interleaved)), softmax_scale
     p.device = first.device
-    p.held = held
+    p.new_rows = axis if packed else p.B * axis
+    p.made_for = {name: (t.shape, t.stride(), t.dtype, t.device) for name, t in given.items()}
+    p.held, p.ref = held, ctypes.byref(p)
     return p
 
 
@@ -354,14 +358,34 @@ def _kv_dtype(t):
     return AA_FP32 if t.dtype == torch.float32 else AA_BF16
 
 
-def _kv_call(fn, p, tensors, strides, args, stream):
-    """Calls fn on the device of p's tensors; tensors are checked against what p was made for."""
-    for t, field in zip(tensors, strides):
-        if t is not None and (t.device != p.device or field and tuple(_kv_strides(t, bool(p.cu_seqlens))) != tuple(getattr(p, field))):
-            raise ValueError("a tensor on %s with strides %s, where the params were made for %s%s"
-                             % (t.device, t.stride(), p.device, " and " + str(tuple(getattr(p, field))) if field else ""))
-    with torch.cuda.device(p.device):
-        _check(fn(ctypes.byref(p), *args, _stream(stream)))
+def _kv_check(p, name, t):
+    """A tensor of a call against the one that p was made for: shape, type, strides and device decide what the kernels touch."""
+    if t is None:
+        return None
+    shape, strides, dtype, device = p.made_for.get(name, (None,) * 4)
+    if t.shape != shape or t.dtype != dtype or t.device != device or (
+            t.stride() != strides and tuple(_kv_strides(t, len(shape) == 3)) != tuple(getattr(p, _KV_FIELDS[name]))):
+        raise ValueError("%s: %s %s strides %s on %s, but the params were made for %s %s strides %s on %s"
+                         % (name, tuple(t.shape), t.dtype, t.stride(), t.device, shape and tuple(shape), dtype, strides, device))
+    return t.data_ptr()
+
+
+def _kv_call(fn, p, stream, *args):
+    """Calls fn with p's device as the current one; a decode step is a few microseconds on the GPU, so the way there is kept short."""
+    at = p.device.index
+    if at is None:
+        raise ValueError("the tensors are on %s: the kernels need a GPU" % p.device)
+    if torch.cuda.current_device() == at:
+        rc = fn(p.ref, *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(at):
+            rc = fn(p.ref, *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+    if rc != AA_OK:
+        raise AnchorError(rc)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def kv_attn_workspace_bytes(p: aa_kv_params) -> int:
@@ -373,26 +397,30 @@ def kv_attn_workspace_bytes(p: aa_kv_params) -> int:
 def kv_append(p, q, k, v, inv_freq=None, positions=None, q_out=None, k_out=None, stream=None):
     """Turn the new queries and keys by their position (q_out, k_out) and store keys and values in the cache's pages.
     inv_freq float32 [rot_dim // 2]; positions int32, one a new token ([B, n] or packed), None: its place in the sequence."""
-    if p.rot_dim and (inv_freq is None or inv_freq.dtype != torch.float32 or inv_freq.numel() != p.rot_dim // 2 or not inv_freq.is_contiguous()):
-        raise ValueError("inv_freq: contiguous float32 [%d] expected" % (p.rot_dim // 2))
-    if positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous()
-                                  or positions.numel() != (p.total_tokens if p.cu_seqlens else p.B * p.N)):
-        raise ValueError("positions: contiguous int32, one a new token, expected")
-    _kv_call(_lib.kv_append, p, (q, k, v, q_out, k_out, inv_freq, positions),
-             ("q_stride", "k_stride", "v_stride", "o_stride", "ko_stride", None, None),
-             (_ptr(q), _ptr(k), _ptr(v), _ptr(inv_freq), _ptr(positions), _ptr(q_out), _ptr(k_out)), stream)
+    at = [_kv_check(p, *x) for x in (("q", q), ("k", k), ("v", v), ("out", q_out), ("k_out", k_out))]
+    if p.rot_dim and (inv_freq is None or inv_freq.dtype != torch.float32 or inv_freq.numel() != p.rot_dim // 2
+                      or not inv_freq.is_contiguous() or inv_freq.device != p.device):
+        raise ValueError("inv_freq: contiguous float32 [%d] on %s expected" % (p.rot_dim // 2, p.device))
+    if positions is not None and (positions.dtype != torch.int32 or not positions.is_contiguous() or positions.device != p.device
+                                  or positions.numel() != p.new_rows):
+        raise ValueError("positions: contiguous int32 on %s, one a new token (%d), expected" % (p.device, p.new_rows))
+    _kv_call(_lib.kv_append, p, stream, at[0], at[1], at[2], _at(inv_freq), _at(positions), at[3], at[4])
 
 
 def kv_attn(p, q, out, lse=None, ws=None, stream=None):
-    """Attention of the new queries over the cached tokens that they see; ws: kv_attn_workspace_bytes(p) bytes, of this call alone
-    while it runs."""
-    _kv_call(_lib.kv_attn, p, (q, out, lse, ws), ("q_stride", "o_stride", None, None),
-             (_ptr(q), _ptr(out), _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()), stream)
+    """Attention of the new queries over the cached tokens that they see.  lse float32 [rows]; ws: kv_attn_workspace_bytes(p)
+    bytes, of this call alone while it runs."""
+    at_q, at_out = _kv_check(p, "q", q), _kv_check(p, "out", out)
+    if lse is not None and (lse.dtype != torch.float32 or lse.numel() != p.Hq * p.new_rows or not lse.is_contiguous() or lse.device != p.device):
+        raise ValueError("lse: contiguous float32 [%d] on %s expected" % (p.Hq * p.new_rows, p.device))
+    if ws is not None and (ws.device != p.device or not ws.is_contiguous()):
+        raise ValueError("ws: contiguous on %s expected" % p.device)
+    _kv_call(_lib.kv_attn, p, stream, at_q, at_out, _at(lse), _at(ws), 0 if ws is None else ws.numel() * ws.element_size())
 
 
 def kv_read(p, k_out=None, v_out=None, stream=None):
     """Copy the rows of every sequence's new tokens out of the cache (4 bits: their values)."""
-    _kv_call(_lib.kv_read, p, (k_out, v_out), ("k_stride", "v_stride"), (_ptr(k_out), _ptr(v_out)), stream)
+    _kv_call(_lib.kv_read, p, stream, _kv_check(p, "k", k_out), _kv_check(p, "v", v_out))
 
 
 def default_scale(d: int) -> float:

@@ -1,24 +1,117 @@
 // kv_append and kv_read: rows of new tokens into the pages of the cache (rotated on the way) and out of them.
+//
+// Memory traffic is all that they cannot do without: every row is read once and written once or twice, at some six operations an
+// element.  A work-group takes four tokens (one where there are few): each of its waves works out where a token lies and the cosines and
+// sines of its position, one angle a lane, for all heads; then the threads take 16 bytes of a row each, the rows of a token that one
+// thread meets being in flight together.
+#include <type_traits>
+
 #include "aa_kv.h"
 
 namespace aa {
 namespace {
 
 using u32x4 = __attribute__((ext_vector_type(4))) unsigned;
+using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 
-template <class T> struct Vec;                  // 16 bytes of a row
-template <> struct Vec<float> { static constexpr int n = 4; };
-template <> struct Vec<__bf16> { static constexpr int n = 8; };
+template <class T> constexpr int kVec = 16 / (int)sizeof(T);       // elements of 16 bytes
 
-template <class T> __device__ __forceinline__ void load16(const T* p, float* x) {
-    union { u32x4 u; T t[Vec<T>::n]; } v;
-    v.u = *(const u32x4*)p;
-    for (int i = 0; i < Vec<T>::n; ++i) x[i] = (float)v.t[i];
+template <class T> __device__ __forceinline__ void unpack(u32x4 u, float* x) {
+    union { u32x4 u; T t[kVec<T>]; } v;
+    v.u = u;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) x[i] = (float)v.t[i];
 }
-template <class T> __device__ __forceinline__ void store16(T* p, const float* x) {
-    union { u32x4 u; T t[Vec<T>::n]; } v;
-    for (int i = 0; i < Vec<T>::n; ++i) v.t[i] = (T)x[i];
-    *(u32x4*)p = v.u;
+template <class T> __device__ __forceinline__ u32x4 pack(const float* x) {
+    union { u32x4 u; T t[kVec<T>]; } v;
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) v.t[i] = (T)x[i];
+    return v.u;
+}
+
+// Cosine and sine of x, |x| <= pi / 4, by their series: the first term left out is below 2^-24 (float) or 2^-54 (double) of the result.
+__device__ __forceinline__ void series(float x, float* c, float* s) {
+    const float y = x * x;
+    *c = 1.f + y * (-1.f / 2 + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320 + y * (-1.f / 3628800)))));
+    *s = x + x * y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880))));
+}
+__device__ __forceinline__ void series(double x, double* c, double* s) {
+    const double y = x * x;
+    *c = 1. + y * (-1. / 2 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 + y * (-1. / 3628800 +
+              y * (1. / 479001600 + y * (-1. / 87178291200. + y * (1. / 20922789888000.))))))));
+    *s = x + x * y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880 + y * (-1. / 39916800 +
+              y * (1. / 6227020800. + y * (-1. / 1307674368000.)))))));
+}
+
+// Cosine and sine of the angle t.  The angle and what is left of it after whole quarter turns are 64-bit numbers (a position of a million
+// leaves 32 bits four digits); 32 bits are enough from there on for results in 32 bits.
+template <class S> __device__ __forceinline__ void cos_sin(double t, S* c, S* s) {
+    const double turns = rint(t * 0.63661977236758134308);
+    double r = fma(-turns, 1.57079632679489661923, t);
+    r = fma(-turns, 6.12323399573676603587e-17, r);                // pi / 2 = 1.57..923 + 6.12..e-17
+    S a, b;
+    series((S)r, &a, &b);
+    const int quarter = (int)(turns - 4. * floor(turns * 0.25));
+    const S x = quarter & 1 ? b : a, y = quarter & 1 ? a : b;
+    *c = quarter == 1 || quarter == 2 ? -x : x;
+    *s = quarter >= 2 ? -y : y;
+}
+
+// y as a float that is on y's side of every number of a few bits: towards zero, with the last bit set if that lost anything.
+__device__ __forceinline__ float to_odd(double y) {
+    const float f = (float)y;
+    const double back = (double)f;
+    unsigned u = __float_as_uint(f);
+    if (back != y) u = (fabs(back) > fabs(y) ? u - 1 : u) | 1u;    // NaN: u | 1, a NaN still
+    return __uint_as_float(u);
+}
+
+// Eight channels of one lane as 4-bit codes, and the scale byte of the 32 that four neighbouring lanes hold.
+__device__ __forceinline__ unsigned to_fp4(const float* x, int* byte) {
+    unsigned top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const unsigned m = __float_as_uint(x[e]) & 0x7fffffffu;
+        top = m > top ? m : top;
+    }
+#pragma unroll
+    for (int s = 1; s < kFp4Group / 8; s *= 2) {
+        const unsigned o = __shfl_xor(top, s);
+        top = o > top ? o : top;
+    }
+    *byte = fp4_scale_byte(top);
+    const float scale = __uint_as_float((unsigned)(*byte == 255 ? 127 : *byte) << 23);
+    unsigned codes = 0;                                             // the instruction rounds to even and cuts to 6
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+    return *byte == 255 ? 0u : codes;
+}
+
+// A new token: its sequence, its number there, its place in the cache.
+struct Token { int b, i, page, in; long long row0, j; };
+__device__ __forceinline__ Token token_of(const KvArgs& a, long long row) {
+    Token t;
+    t.b = 0;
+    if (!a.cu) {
+        t.b = (int)(row / a.N);
+    } else {
+        for (int at = 0; at < a.B; at += 64) {      // sequences that end at or before the row
+            const int i = at + (threadIdx.x & 63);
+            t.b += __popcll(__ballot(i < a.B && a.cu[i + 1] <= row));
+        }
+    }
+    t.i = -1;
+    if (t.b >= a.B) return t;
+    const KvSeq sq = kv_seq(a, t.b);
+    if (row < sq.row0 || row - sq.row0 >= sq.n) return t;
+    t.i = (int)(row - sq.row0);
+    t.row0 = sq.row0;
+    t.j = (long long)a.kv_len[t.b] - sq.n + t.i;
+    t.page = kv_page(a, t.b, t.j);
+    t.in = (int)t.j & ((1 << a.page_shift) - 1);
+    return t;
 }
 
 struct AppendArgs {
@@ -29,134 +122,214 @@ struct AppendArgs {
     void *q_out, *k_out;
 };
 
-// Which sequence a row of the token axis belongs to: B if none.
-__device__ __forceinline__ int seq_of_row(const KvArgs& a, long long row) {
-    if (!a.cu) return (int)(row / a.N);
-    int b = 0;
-    for (int at = 0; at < a.B; at += 64) {      // sequences that end at or before the row
-        const int i = at + (threadIdx.x & 63);
-        b += __popcll(__ballot(i < a.B && a.cu[i + 1] <= row));
-    }
-    return b;
+constexpr int kInFlight = 3;                    // rows of a token that a thread loads before it goes on
+enum { kNoPairs, kHalves, kNeighbours };        // which channels are turned together
+
+__device__ __forceinline__ long long uniform(long long x) {
+    return (long long)(unsigned)__builtin_amdgcn_readfirstlane((int)x) |
+           (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
 }
 
-// One work-group a token: cosines and sines of its position first, once for all heads; then 16 bytes of a head's row a thread.
-template <class T, bool FP4, int D>
+template <class T, bool FP4, int D, int PAIRS, int TOKENS>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
-    constexpr int V = Vec<T>::n, LANES = D / V;
-    __shared__ double s_cos[D / 2], s_sin[D / 2];
+    constexpr int V = kVec<T>, LANES = D / V, ROWS = 256 / LANES, item = sizeof(T);
+    using S = typename std::conditional<FP4, double, float>::type;
+    __shared__ S s_cs[TOKENS][D / 2][2];
+    __shared__ Token s_tok[TOKENS];
     const KvArgs& a = p.a;
-    const long long row = blockIdx.x;
-    const int b = seq_of_row(a, row);
-    if (b >= a.B) return;
-    const KvSeq sq = kv_seq(a, b);
-    const int i = (int)(row - sq.row0);
-    if (i < 0 || i >= sq.n) return;
-    const long long j = (long long)a.kv_len[b] - sq.n + i;
-    const double pos = p.positions ? (double)p.positions[row] : (double)j;
-    for (int f = threadIdx.x; f < a.rot / 2; f += 256) {
-        double sn, cs;
-        sincos(pos * (double)p.inv_freq[f], &sn, &cs);
-        s_cos[f] = cs; s_sin[f] = sn;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long row_first = (long long)blockIdx.x * TOKENS;
+    if (wave < TOKENS) {
+        Token t;
+        t.i = -1;
+        if (row_first + wave < a.total) t = token_of(a, row_first + wave);
+        if (lane == 0) s_tok[wave] = t;
+        if (PAIRS != kNoPairs && t.i >= 0 && lane < a.rot / 2) {
+            const double pos = p.positions ? (double)p.positions[row_first + wave] : (double)t.j;
+            cos_sin<S>(pos * (double)p.inv_freq[lane], &s_cs[wave][lane][0], &s_cs[wave][lane][1]);
+        }
     }
     __syncthreads();
-    const int page = kv_page(a, b, j), in = (int)j & ((1 << a.page_shift) - 1);
-    const int nq = p.q_out ? a.Hq : 0, nk = p.k ? a.Hkv : 0;
-    for (int r = threadIdx.x / LANES; r < nq + 2 * nk; r += 256 / LANES) {
-        const int c = threadIdx.x % LANES * V;
-        const bool is_q = r < nq, is_v = r >= nq + nk;
-        const int h = is_q ? r : is_v ? r - nq - nk : r - nq;
-        const T* src = (const T*)(is_q ? p.q : is_v ? p.v : p.k) +
-                       kv_row(a, is_q ? a.qs : is_v ? a.vs : a.ks, b, sq.row0, i, h);
-        float x[V];
-        double y[V];
-        load16(src + c, x);
-        for (int e = 0; e < V; ++e) y[e] = x[e];
-        if (!is_v && c < a.rot) {
-            float z[V];
-            const int half = a.rot / 2, other = a.interleaved ? c : c < half ? c + half : c - half;
-            load16(src + other, z);
-            for (int e = 0; e < V; ++e) {
-                const int f = a.interleaved ? (c + e) / 2 : (c < half ? c : c - half) + e;
-                const bool first = a.interleaved ? !(e & 1) : c < half;
-                const double mate = a.interleaved ? x[e ^ 1] : z[e];
-                y[e] = first ? x[e] * s_cos[f] - mate * s_sin[f] : x[e] * s_cos[f] + mate * s_sin[f];
-            }
+    const int nq = p.q_out ? a.Hq : 0, nk = p.k ? a.Hkv : 0, rows = nq + 2 * nk;
+    const int c = threadIdx.x % LANES * V, half = a.rot / 2;
+    const bool turn = PAIRS != kNoPairs && c < a.rot, upper = PAIRS == kHalves && c >= half;
+    const int other = !turn ? 0 : PAIRS == kHalves ? (upper ? -half : half) : 0;         // the pair's other chunk
+    const int f0 = !turn ? 0 : PAIRS == kNeighbours ? c / 2 : upper ? c - half : c;
+    for (int r0 = threadIdx.x / LANES + ROWS * kInFlight * blockIdx.y; r0 < rows + threadIdx.x / LANES;
+         r0 += ROWS * kInFlight * gridDim.y) {
+        // where a thread's rows lie from the token's on, in bytes
+        bool is_q[kInFlight], is_v[kInFlight], there[kInFlight];
+        long long from[kInFlight], to[kInFlight], pool[kInFlight];
+        int head[kInFlight];
+#pragma unroll
+        for (int u = 0; u < kInFlight; ++u) {
+            const int r = r0 + u * ROWS < rows ? r0 + u * ROWS : rows - 1;
+            there[u] = r0 + u * ROWS < rows;
+            is_q[u] = r < nq;
+            is_v[u] = r >= nq + nk;
+            const int h = is_q[u] ? r : is_v[u] ? r - nq - nk : r - nq;
+            head[u] = h;
+            from[u] = (long long)h * (is_q[u] ? a.qs[1] : is_v[u] ? a.vs[1] : a.ks[1]) + c;
+            to[u] = (long long)h * (is_q[u] ? a.os[1] : a.kos[1]) + c;
+            pool[u] = (long long)h * (is_v[u] ? a.vcs[1] : a.kcs[1]) + (FP4 ? c / 2 : c);
         }
-        float w[V];
-        for (int e = 0; e < V; ++e) w[e] = (float)y[e];
-        if (is_q) store16((T*)p.q_out + kv_row(a, a.os, b, sq.row0, i, h) + c, w);
-        if (is_q) continue;
-        if (!is_v && p.k_out) store16((T*)p.k_out + kv_row(a, a.kos, b, sq.row0, i, h) + c, w);
-        const long long* cs = is_v ? a.vcs : a.kcs;
-        char* pool = is_v ? a.vc : a.kc;
-        if constexpr (!FP4) {
-            if (page >= 0) store16((T*)pool + page * cs[0] + h * cs[1] + in * cs[2] + c, w);
-        } else {
-            uint64_t top = 0;
-            for (int e = 0; e < V; ++e) {
-                const uint64_t m = (uint64_t)__double_as_longlong(y[e]) & 0x7fffffffffffffffull;
-                top = m > top ? m : top;
+#pragma unroll 1
+        for (int tk = 0; tk < TOKENS; ++tk) {
+            const int i = __builtin_amdgcn_readfirstlane(s_tok[tk].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk].b);
+            if (i < 0) continue;
+            const int page = __builtin_amdgcn_readfirstlane(s_tok[tk].page), in = __builtin_amdgcn_readfirstlane(s_tok[tk].in);
+            const long long row0 = uniform(s_tok[tk].row0);
+            const T* q = (const T*)p.q + kv_row(a, a.qs, b, row0, i, 0);
+            const T* k = (const T*)p.k + kv_row(a, a.ks, b, row0, i, 0);
+            const T* v = (const T*)p.v + kv_row(a, a.vs, b, row0, i, 0);
+            u32x4 x[kInFlight], z[kInFlight];
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                const T* src = (is_q[u] ? q : is_v[u] ? v : k) + from[u];
+                x[u] = *(const u32x4*)src;
+                if (PAIRS == kHalves) z[u] = *(const u32x4*)(src + other);
             }
-            for (int s = 1; s < kFp4Group / V; s *= 2) {
-                const uint64_t o = __shfl_xor((unsigned long long)top, s);
-                top = o > top ? o : top;
+            float cs[V], sn[V];
+            if (PAIRS != kNoPairs && !FP4) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int f = f0 + (PAIRS == kNeighbours ? e / 2 : e);
+                    cs[e] = s_cs[tk][f][0];
+                    sn[e] = s_cs[tk][f][1];
+                    if (PAIRS == kNeighbours ? !(e & 1) : !upper) sn[e] = -sn[e];
+                }
             }
-            const int byte = fp4_scale_byte(top);
-            const double inv = fp4_inverse_scale(byte == 255 ? 127 : byte);
-            unsigned codes = 0;
-            for (int e = 0; e < V; ++e) codes |= fp4_code(y[e] * inv) << (4 * e);
-            if (page >= 0) {
-                *(unsigned*)(pool + page * cs[0] + h * cs[1] + in * cs[2] + c / 2) = codes;
-                const long long* ss = is_v ? a.vss : a.kss;
-                if (c % kFp4Group == 0)
-                    (is_v ? a.vsc : a.ksc)[page * ss[0] + h * ss[1] + c / kFp4Group * ss[2] + in] = (unsigned char)byte;
+            T* qo = (T*)p.q_out + kv_row(a, a.os, b, row0, i, 0);
+            T* ko = (T*)p.k_out + kv_row(a, a.kos, b, row0, i, 0);
+            char* kc = a.kc + (page * a.kcs[0] + in * a.kcs[2]) * (FP4 ? 1 : item);
+            char* vc = a.vc + (page * a.vcs[0] + in * a.vcs[2]) * (FP4 ? 1 : item);
+#pragma unroll
+            for (int u = 0; u < kInFlight; ++u) {
+                float y[V], m[V];
+                unpack<T>(x[u], y);
+                if (PAIRS == kHalves) {
+                    unpack<T>(z[u], m);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) m[e] = y[e ^ 1];
+                }
+                const bool turned = turn && !is_v[u];
+                u32x4 w = x[u];
+                if constexpr (!FP4) {
+                    if (PAIRS != kNoPairs) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) y[e] = fmaf(m[e], sn[e], y[e] * cs[e]);
+                        const u32x4 r = pack<T>(y);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = turned ? r[e] : w[e];
+                    }
+                } else if (turned) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int f = f0 + (PAIRS == kNeighbours ? e / 2 : e);
+                        const S c64 = s_cs[tk][f][0], s64 = (PAIRS == kNeighbours ? !(e & 1) : !upper) ? -s_cs[tk][f][1] : s_cs[tk][f][1];
+                        y[e] = is_q[u] ? fmaf(m[e], (float)s64, y[e] * (float)c64) : to_odd(fma((double)m[e], s64, y[e] * c64));
+                    }
+                    w = pack<T>(y);
+                }
+                if (!there[u]) continue;
+                if (is_q[u]) {
+                    *(u32x4*)(qo + to[u]) = w;
+                    continue;
+                }
+                if (p.k_out && !is_v[u]) *(u32x4*)(ko + to[u]) = w;
+                if (page < 0) continue;
+                if constexpr (!FP4) {
+                    *(u32x4*)((is_v[u] ? vc : kc) + pool[u] * item) = w;
+                } else {
+                    int byte;
+                    *(unsigned*)((is_v[u] ? vc : kc) + pool[u]) = to_fp4(y, &byte);
+                    if (c % kFp4Group) continue;
+                    unsigned char* sc = is_v[u] ? a.vsc + page * a.vss[0] + head[u] * a.vss[1] + c / kFp4Group * a.vss[2]
+                                                : a.ksc + page * a.kss[0] + head[u] * a.kss[1] + c / kFp4Group * a.kss[2];
+                    sc[in] = (unsigned char)byte;
+                }
             }
         }
     }
 }
 
-// One work-group a token: the cached rows of its heads.
 template <class T, bool FP4, int D>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a, T* k_out, T* v_out) {
-    constexpr int V = Vec<T>::n, LANES = D / V;
-    const long long row = blockIdx.x;
-    const int b = seq_of_row(a, row);
-    if (b >= a.B) return;
-    const KvSeq sq = kv_seq(a, b);
-    const int i = (int)(row - sq.row0);
-    if (i < 0 || i >= sq.n) return;
-    const long long j = (long long)a.kv_len[b] - sq.n + i;
-    const int page = kv_page(a, b, j), in = (int)j & ((1 << a.page_shift) - 1);
-    for (int r = threadIdx.x / LANES; r < 2 * a.Hkv; r += 256 / LANES) {
-        const int c = threadIdx.x % LANES * V, h = r >> 1;
-        const bool is_v = r & 1;
-        T* out = is_v ? v_out : k_out;
-        if (!out) continue;
-        const long long* cs = is_v ? a.vcs : a.kcs;
-        const char* pool = is_v ? a.vc : a.kc;
-        float x[V] = {};
-        if (page >= 0) {
-            if constexpr (!FP4) {
-                load16((const T*)pool + page * cs[0] + h * cs[1] + in * cs[2] + c, x);
+    constexpr int V = kVec<T>, LANES = D / V, ROWS = 256 / LANES, TOKENS = 4, item = sizeof(T);
+    __shared__ Token s_tok[TOKENS];
+    const int wave = threadIdx.x >> 6;
+    const long long row = (long long)blockIdx.x * TOKENS + wave;
+    Token mine;
+    mine.i = -1;
+    if (row < a.total) mine = token_of(a, row);
+    if ((threadIdx.x & 63) == 0) s_tok[wave] = mine;
+    __syncthreads();
+    const int c = threadIdx.x % LANES * V, nk = k_out ? a.Hkv : 0, rows = nk + (v_out ? a.Hkv : 0);
+    for (int r = threadIdx.x / LANES; r < rows; r += ROWS) {
+        const bool is_v = r >= nk;
+        const int h = is_v ? r - nk : r;
+        const long long pool = (long long)h * (is_v ? a.vcs[1] : a.kcs[1]) + (FP4 ? c / 2 : c);
+        const long long to = (long long)h * (is_v ? a.vs[1] : a.ks[1]) + c;
+        const long long scale_at = FP4 ? (long long)h * (is_v ? a.vss[1] : a.kss[1]) + c / kFp4Group * (is_v ? a.vss[2] : a.kss[2]) : 0;
+        u32x4 x[TOKENS];
+        unsigned byte[TOKENS];
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) {
+            const int page = __builtin_amdgcn_readfirstlane(s_tok[t].page), in = __builtin_amdgcn_readfirstlane(s_tok[t].in);
+            x[t] = u32x4{0, 0, 0, 0};
+            byte[t] = 127;
+            if (__builtin_amdgcn_readfirstlane(s_tok[t].i) < 0 || page < 0) continue;
+            const char* kc = a.kc + (page * a.kcs[0] + in * a.kcs[2]) * (FP4 ? 1 : item);
+            const char* vc = a.vc + (page * a.vcs[0] + in * a.vcs[2]) * (FP4 ? 1 : item);
+            if constexpr (FP4) {
+                x[t][0] = *(const unsigned*)((is_v ? vc : kc) + pool);
+                byte[t] = ((is_v ? a.vsc + page * a.vss[0] : a.ksc + page * a.kss[0]) + in)[scale_at];
             } else {
-                const unsigned codes = *(const unsigned*)(pool + page * cs[0] + h * cs[1] + in * cs[2] + c / 2);
-                const long long* ss = is_v ? a.vss : a.kss;
-                const int byte = (is_v ? a.vsc : a.ksc)[page * ss[0] + h * ss[1] + c / kFp4Group * ss[2] + in];
-                for (int e = 0; e < V; ++e) x[e] = fp4_value(codes >> (4 * e) & 15, byte);
+                x[t] = *(const u32x4*)((is_v ? vc : kc) + pool * item);
             }
         }
-        store16(out + kv_row(a, is_v ? a.vs : a.ks, b, sq.row0, i, h) + c, x);
+#pragma unroll
+        for (int t = 0; t < TOKENS; ++t) {
+            const int i = __builtin_amdgcn_readfirstlane(s_tok[t].i), b = __builtin_amdgcn_readfirstlane(s_tok[t].b);
+            if (i < 0) continue;
+            const long long row0 = uniform(s_tok[t].row0);
+            u32x4 w = x[t];
+            if constexpr (FP4) {
+                union { u32x4 u; bf16x2 b[4]; } v;
+                const float scale = __uint_as_float(byte[t] << 23);
+                v.b[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[t][0], scale, 0);
+                v.b[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[t][0], scale, 1);
+                v.b[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[t][0], scale, 2);
+                v.b[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x[t][0], scale, 3);
+                w = v.u;
+            }
+            T* k = k_out + kv_row(a, a.ks, b, row0, i, 0);
+            T* v = v_out + kv_row(a, a.vs, b, row0, i, 0);
+            *(u32x4*)((is_v ? v : k) + to) = w;
+        }
     }
 }
 
+template <class T, bool FP4, int D, int PAIRS>
+int run_pairs(const AppendArgs& p, hipStream_t st) {
+    constexpr int PASS = 256 / (D / kVec<T>) * kInFlight;          // rows of a token in one pass of a work-group
+    const int rows = (p.q_out ? p.a.Hq : 0) + (p.k ? 2 * p.a.Hkv : 0);
+    // Few tokens: a work-group a pass of a token's rows, so that none waits for a second one.
+    if (p.a.total < 1024) {
+        const int passes = (rows + PASS - 1) / PASS;
+        return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1>, dim3((unsigned)p.a.total, passes < 64 ? passes : 64), dim3(256), 0, st, p);
+    }
+    return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4>, dim3((unsigned)((p.a.total + 3) / 4)), dim3(256), 0, st, p);
+}
 template <class T, bool FP4, int D>
 int run_append(const AppendArgs& p, hipStream_t st) {
-    return (int)launch_kernel(kv_append_kernel<T, FP4, D>, dim3((unsigned)p.a.total), dim3(256), 0, st, p);
+    return !p.a.rot ? run_pairs<T, FP4, D, kNoPairs>(p, st) : p.a.interleaved ? run_pairs<T, FP4, D, kNeighbours>(p, st)
+                                                            : run_pairs<T, FP4, D, kHalves>(p, st);
 }
 template <class T, bool FP4, int D>
 int run_read(const KvArgs& a, void* k, void* v, hipStream_t st) {
-    return (int)launch_kernel(kv_read_kernel<T, FP4, D>, dim3((unsigned)a.total), dim3(256), 0, st, a, (T*)k, (T*)v);
+    return (int)launch_kernel(kv_read_kernel<T, FP4, D>, dim3((unsigned)((a.total + 3) / 4)), dim3(256), 0, st, a, (T*)k, (T*)v);
 }
 
 }  // namespace

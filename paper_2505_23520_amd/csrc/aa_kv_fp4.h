@@ -14,30 +14,16 @@ namespace aa {
 
 constexpr int kFp4Group = 32;               // channels with one scale
 
-// `top`: the bits of the largest magnitude of a group, as of a double (NaN above infinity above numbers).
+// `top`: the bits of the largest magnitude of a group, as of a float (NaN above infinity above numbers).
 // The scale byte: 127 + the least e of [-120, 125] with top <= 7 * 2^e, or 255 if the group holds a NaN or an infinity.
 // 7: a largest value between 6 and 7 loses less by being cut to 6 than the group loses by the next coarser scale (root mean square
 // error of normal values 0.1119; with 6 0.1154, with 8 0.1150; heavier tails 0.129 / 0.139 / 0.131).
 // The bounds keep every code's value a normal bf16 number.
-AA_HD int fp4_scale_byte(uint64_t top) {
-    const int ex = (int)(top >> 52);
-    if (ex == 0x7ff) return 255;
-    const int e = ex - 1023 - 2 + ((top & 0xfffffffffffffull) > 0xc000000000000ull);
+AA_HD int fp4_scale_byte(uint32_t top) {
+    const int ex = (int)(top >> 23);
+    if (ex == 255) return 255;
+    const int e = ex - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
     return 127 + (e < -120 ? -120 : e > 125 ? 125 : e);
-}
-
-// 2^(127 - byte) in 64 bits
-AA_HD double fp4_inverse_scale(int byte) {
-    union { uint64_t u; double x; } v;
-    v.u = (uint64_t)(1023 + 127 - byte) << 52;
-    return v.x;
-}
-
-// Nearest code of x (already divided by the scale), ties to the even code; what is above 6 becomes 6.
-AA_HD unsigned fp4_code(double x) {
-    const double a = x < 0 ? -x : x;
-    const unsigned c = (a > 0.25) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0);
-    return c | (x < 0 ? 8u : 0u);
 }
 
 // The value of a code under a scale byte.

@@ -124,31 +124,28 @@ def test_binding_rejects(api):
             api.kv_append(p, *args)
 
 
-def test_fp4_code_on_the_host(tmp_path):
-    """fp4_scale_byte, fp4_code and fp4_value against every code and exponent tried out."""
+def test_fp4_scale_on_the_host(tmp_path):
+    """fp4_scale_byte and fp4_value against every exponent tried out and the format's table."""
     from kv_util import fp4_pack, fp4_values
     src, exe = tmp_path / "f.cpp", str(tmp_path / "f")
     src.write_text('''#include "%s/paper_2505_23520_amd/csrc/aa_kv_fp4.h"
 #include <stdio.h>
-#include <string.h>
 int main() {
-    double x[32];
-    while (fread(x, 8, 32, stdin) == 32) {
-        uint64_t top = 0;
-        for (int i = 0; i < 32; ++i) { uint64_t u; memcpy(&u, x + i, 8); u &= 0x7fffffffffffffffull; if (u > top) top = u; }
-        const int byte = aa::fp4_scale_byte(top);
-        for (int i = 0; i < 32; ++i) {
-            const unsigned c = byte == 255 ? 0 : aa::fp4_code(x[i] * aa::fp4_inverse_scale(byte));
-            printf("%%.17g\\n", (double)aa::fp4_value(c, byte));
-        }
-    }
+    unsigned u;
+    while (fread(&u, 4, 1, stdin) == 1) printf("%%d\\n", aa::fp4_scale_byte(u));
+    for (int b = 7; b <= 255; b += b == 252 ? 3 : 1)
+        for (unsigned c = 0; c < 16; ++c) printf("%%.17g\\n", (double)aa::fp4_value(c, b));
 }''' % ROOT)
     subprocess.check_call(["g++", "-O2", "-std=c++17", str(src), "-o", exe])
     gen = torch.Generator().manual_seed(1)
-    x = torch.randn(400, 32, generator=gen, dtype=torch.float64)
-    x = torch.cat([x, (x * 8).round() / 8, (x[:100] * 4).round(), x[:50] * 2.0 ** -125, x[:50] * 2.0 ** 125, torch.zeros(1, 32)])
-    x[3, 4], x[5, 6], x[7, 8] = float("inf"), float("nan"), -float("inf")
+    x = torch.randn(400, generator=gen).abs()
+    x = torch.cat([x, x * 2.0 ** -125, x * 2.0 ** 126, 7 * torch.exp2(torch.arange(-125.0, 126.0)), torch.tensor([0.0, float("inf"), float("nan"), 1e-45])])
+    x = torch.cat([x, torch.nextafter(x, torch.tensor(float("inf"))), torch.nextafter(x, torch.tensor(0.0))])
     got = subprocess.run([exe], input=x.numpy().tobytes(), capture_output=True, check=True).stdout.split()
-    got = torch.tensor([float(t) for t in got], dtype=torch.float64).view(-1, 32)
-    want = fp4_values(*fp4_pack(x))
-    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(), want.nan_to_num())
+    scales = fp4_pack(torch.stack([x.double()] + [torch.zeros(x.numel(), dtype=torch.float64)] * 31, dim=1))[1]
+    assert [int(t) for t in got[:x.numel()]] == scales[:, 0].tolist()
+    vals = torch.tensor([float(t) for t in got[x.numel():]], dtype=torch.float64).view(-1, 16)
+    codes = torch.tensor([i | j << 4 for i, j in zip(range(0, 16, 2), range(1, 16, 2))] * 2, dtype=torch.uint8)
+    for byte, row in zip(list(range(7, 253)) + [255], vals):
+        want = fp4_values(codes, torch.tensor([byte], dtype=torch.uint8))[:16]
+        assert torch.equal(torch.isnan(row), torch.isnan(want)) and torch.equal(row.nan_to_num(), want.nan_to_num())
