@@ -13,7 +13,7 @@
 //                keys 4g .. 4g+3 of each half of the tile, and the sum over keys may run in that order too.  The left operand wants 8 keys of
 //                one channel in a lane; a lane loads D/16 channels of each of its keys and two byte permutations turn four bf16 values.
 // A lane's rows of S^T, O^T, m and the sum are all row lane % 16, so nothing crosses lanes unless a reference is raised.
-#include "aa_kv.h"
+#include "aa_kv_attn.h"
 
 namespace aa {
 namespace {
@@ -25,20 +25,9 @@ using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 
 constexpr int kWaves = 4;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;       // a reference is raised when a score exceeds it by 2^8: weights stay below 256 in 32-bit sums
 
 enum { kRows32, kRows16, kRows4 };  // cached rows: float, bf16, 4 bits
-
-struct AttnArgs {
-    KvArgs a;
-    const void* q;
-    void* out;
-    float *lse, *ws;
-    int splits, chunk, rows, tiles;  // rows of a KV head (N * grp); row tiles
-    float c;                         // sigma * log2 e
-    FastDiv by_hkv, by_splits, by_grp;
-};
 
 template <int F> struct RowType { using type = __bf16; };
 template <> struct RowType<kRows32> { using type = float; };
@@ -282,14 +271,6 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
     }
 }
 
-// Keys that new token i of n of a sequence sees.
-__device__ __forceinline__ int seen(const KvArgs& a, int len, int n, int i) {
-    const long long room = (long long)a.max_pages << a.page_shift;
-    long long x = a.causal ? (long long)len - n + i + 1 : len;
-    if (x > room) x = room;
-    return x < 0 ? 0 : (int)x;
-}
-
 template <int F, int D, int NT>
 __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(AttnArgs p) {
     using T = typename RowType<F>::type;
@@ -298,26 +279,18 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.y;
-    const unsigned rest = p.by_hkv.div(blockIdx.x), hk = blockIdx.x - rest * a.Hkv;
-    const unsigned back = p.by_splits.div(rest), split = rest - back * p.splits;
-    const int r0 = (p.tiles - 1 - (int)back) * R;             // the last rows first: they see the most keys
-    const KvSeq sq = kv_seq(a, b);
-    const int len = a.kv_len[b], rows = sq.n * a.grp;
-    if (r0 >= rows) return;
-    const int last = r0 + R < rows ? r0 + R - 1 : rows - 1;
-    const int see_last = seen(a, len, sq.n, (int)p.by_grp.div(last)), see_first = seen(a, len, sq.n, (int)p.by_grp.div(r0));
-    const int lo = (int)split * p.chunk;
-    if (split && lo >= see_last) return;
-    const int hi = (int)split == p.splits - 1 || see_last - lo < p.chunk ? see_last : lo + p.chunk;
+    AttnPart wp;
+    if (!attn_part<R>(p, wp)) return;
+    const int b = wp.b, hk = wp.hk, r0 = wp.r0, rows = wp.rows, lo = wp.lo, hi = wp.hi;
+    const KvSeq sq = wp.sq;
 
     Rows<F, D, NT> r;
     const int n16 = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = r0 + 16 * n + n16 < rows ? r0 + 16 * n + n16 : rows - 1;
-        const int i = (int)p.by_grp.div(row), h = (int)hk * a.grp + row - i * a.grp;
-        r.see[n] = seen(a, len, sq.n, i);
+        const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+        r.see[n] = seen(a, wp.len, sq.n, i);
         r.m[n] = -INFINITY;
         r.l[n] = 0.f;
         const char* q = (const char*)p.q + kv_row(a, a.qs, b, sq.row0, i, h) * item;
@@ -354,11 +327,11 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
         for (;;) {
             const int k1 = key + kWaves * TK;
             load_tile<F, D>(a, w, k1 < hi ? k1 : key, t1);
-            attend_tile<F, D, NT>(p, t0, hi, see_first, r);
+            attend_tile<F, D, NT>(p, t0, hi, wp.see_first, r);
             if (k1 >= hi) break;
             key = k1 + kWaves * TK;
             load_tile<F, D>(a, w, key < hi ? key : k1, t0);
-            attend_tile<F, D, NT>(p, t1, hi, see_first, r);
+            attend_tile<F, D, NT>(p, t1, hi, wp.see_first, r);
             if (key >= hi) break;
         }
     }
@@ -390,14 +363,14 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) acc[j] += f * s_o[k][x][c0 + j];
         }
-        const int i = (int)p.by_grp.div(row), h = (int)hk * a.grp + row - i * a.grp;
+        const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
         if (p.splits > 1) {
-            const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits + split;
+            const long long at = share_of(p, wp, row);
             float* o = p.ws + at * D + c0;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[j] = acc[j];
             if (c0 == 0) {
-                float* ml = p.ws + (long long)a.B * a.Hkv * p.rows * p.splits * D + at * 2;
+                float* ml = share_sums(p, D) + at * 2;
                 ml[0] = m; ml[1] = sum;
             }
         } else {
@@ -406,7 +379,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[j] = (T)(acc[j] * inv);
             if (p.lse && c0 == 0)
-                p.lse[a.cu ? h * a.total + sq.row0 + i : ((long long)b * a.Hq + h) * a.N + i] =
+                p.lse[lse_of(a, sq, b, h, i)] =
                     sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
         }
     }
@@ -421,7 +394,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.y;
     const unsigned row = p.by_hkv.div(blockIdx.x), hk = blockIdx.x - row * a.Hkv;
     const KvSeq sq = kv_seq(a, b);
-    const int i = (int)p.by_grp.div(row), h = (int)hk * a.grp + row - i * a.grp;
+    const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
     if (i >= sq.n) return;
     // a share wrote this row if its keys begin before those that the row's tile of rows sees end; before those of the row is enough
     const int see = seen(a, a.kv_len[b], sq.n, i);
@@ -429,7 +402,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
     parts = parts > p.splits ? p.splits : parts < 1 ? 1 : parts;
     const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits;
     const float* o = p.ws + at * D;
-    const float* ml = p.ws + (long long)a.B * a.Hkv * p.rows * p.splits * D + at * 2;
+    const float* ml = share_sums(p, D) + at * 2;
     constexpr int E = (D + 63) / 64;
     float m = -INFINITY, l = 0.f, acc[E] = {};
     for (int s = wave; s < parts; s += 4) {
@@ -457,30 +430,34 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
     }
     ((T*)p.out)[kv_row(a, a.os, b, sq.row0, i, h) + c] = (T)(sum == 0.f ? 0.f : x / sum);
     if (p.lse && c == 0)
-        p.lse[a.cu ? h * a.total + sq.row0 + i : ((long long)b * a.Hq + h) * a.N + i] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+        p.lse[lse_of(a, sq, b, h, i)] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
 }
 
-int row_tiles_of(long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+// Rows of a work-group.  Beyond 64 rows with d = 128 and bf16 products: 128 through LDS.
+int tile_rows(long long rows, int d, int dtype) {
+    if (rows > 64 && d == 128 && dtype != 0) return kChunkRows;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
 
 template <int F, int D>
-int run(const AttnArgs& p, hipStream_t st) {
+int run(const AttnArgs& p, int R, hipStream_t st) {
     using T = typename RowType<F>::type;
-    const int nt = row_tiles_of(p.rows);
     const long long x = (long long)p.a.Hkv * p.tiles * p.splits, rows = (long long)p.a.Hkv * p.rows;
     if (x > 0x7fffffffll || (p.splits > 1 && rows > 0x7fffffffll)) return -1;
     const dim3 grid((unsigned)x, p.a.B), block(64 * kWaves);
-    hipError_t e;
-    if (nt == 1) e = launch_kernel(kv_attn_kernel<F, D, 1>, grid, block, 0, st, p);
-    else if (nt == 2) e = launch_kernel(kv_attn_kernel<F, D, 2>, grid, block, 0, st, p);
-    else e = launch_kernel(kv_attn_kernel<F, D, 4>, grid, block, 0, st, p);
-    if (e != hipSuccess || p.splits == 1) return (int)e;
+    int e;
+    if (R == 16) e = (int)launch_kernel(kv_attn_kernel<F, D, 1>, grid, block, 0, st, p);
+    else if (R == 32) e = (int)launch_kernel(kv_attn_kernel<F, D, 2>, grid, block, 0, st, p);
+    else if (R == 64) e = (int)launch_kernel(kv_attn_kernel<F, D, 4>, grid, block, 0, st, p);
+    else e = launch_kv_chunk(p, F == kRows4, grid, st);
+    if (e != (int)hipSuccess || p.splits == 1) return e;
     return (int)launch_kernel(kv_join_kernel<T, D>, dim3((unsigned)rows, p.a.B), dim3(256), 0, st, p);
 }
 
 }  // namespace
 
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, long long longest) {
-    const long long rows = (long long)N * (Hq / Hkv), nt = row_tiles_of(rows), tiles = (rows + 16 * nt - 1) / (16 * nt);
+    const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype), tiles = (rows + R - 1) / R;
     const long long groups = tiles * B * Hkv;
     long long splits = (1024 + groups - 1) / groups;
     if (tiles == 1 && splits < (longest + 2047) / 2048) splits = (longest + 2047) / 2048;
@@ -502,13 +479,13 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     p.q = q; p.out = out; p.lse = lse; p.ws = ws;
     p.splits = sp.splits; p.chunk = sp.chunk;
     p.rows = a.N * a.grp;
-    const int R = 16 * row_tiles_of(p.rows);
+    const int R = tile_rows(p.rows, d, dtype);
     p.tiles = (p.rows + R - 1) / R;
     p.c = a.sigma * kLog2e;
     p.by_hkv.set(a.Hkv); p.by_splits.set(sp.splits); p.by_grp.set(a.grp);
-    if (dtype == 0) return d == 32 ? run<kRows32, 32>(p, st) : d == 64 ? run<kRows32, 64>(p, st) : d == 128 ? run<kRows32, 128>(p, st) : -1;
-    if (format) return d == 64 ? run<kRows4, 64>(p, st) : d == 128 ? run<kRows4, 128>(p, st) : -1;
-    return d == 64 ? run<kRows16, 64>(p, st) : d == 128 ? run<kRows16, 128>(p, st) : -1;
+    if (dtype == 0) return d == 32 ? run<kRows32, 32>(p, R, st) : d == 64 ? run<kRows32, 64>(p, R, st) : d == 128 ? run<kRows32, 128>(p, R, st) : -1;
+    if (format) return d == 64 ? run<kRows4, 64>(p, R, st) : d == 128 ? run<kRows4, 128>(p, R, st) : -1;
+    return d == 64 ? run<kRows16, 64>(p, R, st) : d == 128 ? run<kRows16, 128>(p, R, st) : -1;
 }
 
 }  // namespace aa
