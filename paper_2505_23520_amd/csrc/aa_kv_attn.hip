@@ -13,6 +13,7 @@
 //                keys 4g .. 4g+3 of each half of the tile, and the sum over keys may run in that order too.  The left operand wants 8 keys of
 //                one channel in a lane; a lane loads D/16 channels of each of its keys and two byte permutations turn four bf16 values.
 // A lane's rows of S^T, O^T, m and the sum are all row lane % 16, so nothing crosses lanes unless a reference is raised.
+#include <stdlib.h>
 #include "aa_kv_attn.h"
 
 namespace aa {
@@ -32,91 +33,118 @@ enum { kRows32, kRows16, kRows4 };  // cached rows: float, bf16, 4 bits
 template <int F> struct RowType { using type = __bf16; };
 template <> struct RowType<kRows32> { using type = float; };
 
-// One tile of keys in registers: TT halves of 16 keys.
+// One tile of keys in registers: TT halves of 16 keys, of which the first rows[h] exist and are seen by some row.
 template <int F, int D> struct Tile;
 template <int D> struct Tile<kRows16, D> {
-    static constexpr int TT = 2;
+    static constexpr int TT = 2, words = D / 32;
     u32x4 k[TT][D / 32];
-    unsigned v[TT][4][D / 32];
-    int key;
-    bool there[TT];
+    unsigned v[TT][4][words];
+    int key, rows[TT];
 };
 template <int D> struct Tile<kRows4, D> {
-    static constexpr int TT = 2;
+    static constexpr int TT = 2, words = 1;
     unsigned k[TT][D / 32];
-    unsigned v[TT][4];
+    unsigned v[TT][4][words];
     unsigned ks[TT], vs[TT];
-    int key;
-    bool there[TT];
+    int key, rows[TT];
 };
 template <int D> struct Tile<kRows32, D> {
-    static constexpr int TT = 1;
-    f32x4 k[TT][D / 16];
-    float v[TT][4][D / 16];
-    int key;
-    bool there[TT];
+    static constexpr int TT = 1, words = D / 16;
+    u32x4 k[TT][D / 16];
+    unsigned v[TT][4][words];
+    int key, rows[TT];
 };
 
-template <int N> __device__ __forceinline__ void load_words(const char* p, unsigned* x) {
+// What a wave needs to find a tile: its sequence's pages, the pools from its head on, and a lane's place in 16 keys (bytes).
+struct Where {
+    const_int* table;
+    long long room;
+    int shift, n_pages;
+    const char *k, *v;
+    const unsigned char *ks, *vs;
+    long long k_page, v_page, k_row, v_row, ks_page, vs_page;
+    int k_lane, v_lane[4], ks_lane, vs_lane, k_end, v_end;     // *_end: where the last row's bytes end, from the row's start
+};
+
+// The pages of a tile; -1: none.
+template <int TT> struct Pages { int p[TT]; };
+template <int TT> __device__ __forceinline__ Pages<TT> pages_of(const Where& w, int key) {
+    Pages<TT> x;
+#pragma unroll
+    for (int h = 0; h < TT; ++h) {
+        const int j = key + 16 * h;
+        x.p[h] = j < w.room ? w.table[j >> w.shift] : -1;
+    }
+    return x;
+}
+
+// `bytes` bytes from x on, what is read behind them is 0.  Both are the same for the whole wave and said to be so: the compiler would
+// otherwise take each load through a loop over the lanes' descriptors.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const void* x, int bytes) {
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)x), hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)x >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((uintptr_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+// n rows, `row` bytes apart, of which the last ends `end` bytes from its start.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* x, int n, long long row, int end) {
+    const int bytes = n * (int)row - ((int)row - end);
+    return bytes_at(x, n > 0 ? bytes : 0);
+}
+
+template <int N> __device__ __forceinline__ void load_words(__amdgpu_buffer_rsrc_t rs, int at, unsigned* x) {
     static_assert(N == 1 || N == 2 || N % 4 == 0, "");
     if constexpr (N == 1) {
-        x[0] = *(const unsigned*)p;
+        x[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, at, 0, 0);
     } else if constexpr (N == 2) {
-        const u32x2 u = *(const u32x2*)p;
+        const u32x2 u = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
         x[0] = u[0]; x[1] = u[1];
     } else {
+#pragma unroll
         for (int i = 0; i < N; i += 4) {
-            const u32x4 u = *(const u32x4*)(p + 4 * i);
+            const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(rs, at + 4 * i, 0, 0);
             x[i] = u[0]; x[i + 1] = u[1]; x[i + 2] = u[2]; x[i + 3] = u[3];
         }
     }
 }
 
-// What a wave needs to find a tile: the pools from its head on, and a lane's place in 16 keys.
-struct Where {
-    const int* table;
-    long long room;
-    const char *k, *v;
-    const unsigned char *ks, *vs;
-    unsigned k_lane, v_lane, ks_lane, vs_lane;
-    long long v_row;                 // bytes between rows of values
-};
-
+// Requests a tile, of which keys below hi count.  Rows that do not exist cost no memory traffic and come as zeros: a last tile's values behind
+// the last key, whose weight is 0, may have any bits.
 template <int F, int D>
-__device__ __forceinline__ void load_tile(const KvArgs& a, const Where& w, int key, Tile<F, D>& t) {
+__device__ __forceinline__ void load_tile(const Where& w, int key, int hi, const Pages<Tile<F, D>::TT>& pages, Tile<F, D>& t) {
     t.key = key;
-    constexpr int item = F == kRows32 ? 4 : 2;
+    constexpr int TT = Tile<F, D>::TT;
+    long long pg[TT];
+    int in[TT];
 #pragma unroll
-    for (int h = 0; h < Tile<F, D>::TT; ++h) {
-        const int j = key + 16 * h;
-        int page = -1;
-        if (j < w.room) page = w.table[j >> a.page_shift];
-        t.there[h] = (unsigned)page < (unsigned)a.n_pages;
-        const long long pg = t.there[h] ? page : 0;         // some storage that exists; its keys are masked
-        const int in = j & ((1 << a.page_shift) - 1);
+    for (int h = 0; h < TT; ++h) {
+        const bool there = (unsigned)pages.p[h] < (unsigned)w.n_pages;
+        const int n = hi - (key + 16 * h);
+        pg[h] = there ? pages.p[h] : 0;
+        in[h] = (key + 16 * h) & ((1 << w.shift) - 1);
+        t.rows[h] = !there ? 0 : n < 16 ? n : 16;            // 0 and less: none
+    }
+#pragma unroll
+    for (int h = 0; h < TT; ++h) {
+        const auto k = rows_at(w.k + pg[h] * w.k_page + in[h] * w.k_row, t.rows[h], w.k_row, w.k_end);
         if constexpr (F == kRows4) {
-            const char* k = w.k + pg * a.kcs[0] + in * a.kcs[2];
-            const char* v = w.v + pg * a.vcs[0] + in * a.vcs[2];
-            load_words<D / 32>(k + w.k_lane, t.k[h]);
-            t.ks[h] = w.ks[pg * a.kss[0] + in + w.ks_lane];
-            t.vs[h] = *(const unsigned*)(w.vs + pg * a.vss[0] + in + w.vs_lane);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const char* x = v + (w.v_lane + i * (unsigned)w.v_row);
-                if constexpr (D == 128) t.v[h][i] = *(const unsigned*)x;
-                else t.v[h][i] = *(const unsigned short*)x;
-            }
+            load_words<D / 32>(k, w.k_lane, t.k[h]);
+            const auto sc = bytes_at(w.ks + pg[h] * w.ks_page + in[h], t.rows[h] > 0 ? 0x7fffffff : 0);
+            t.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(sc, w.ks_lane, 0, 0);
         } else {
-            const char* k = w.k + (pg * a.kcs[0] + in * a.kcs[2]) * item;
-            const char* v = w.v + (pg * a.vcs[0] + in * a.vcs[2]) * item;
-            constexpr int steps = D * item / 64;
 #pragma unroll
-            for (int s = 0; s < steps; ++s) {
-                if constexpr (F == kRows32) t.k[h][s] = *(const f32x4*)(k + 64 * s + w.k_lane);
-                else t.k[h][s] = *(const u32x4*)(k + 64 * s + w.k_lane);
-            }
+            for (int s = 0; s < (F == kRows32 ? D / 16 : D / 32); ++s) t.k[h][s] = __builtin_amdgcn_raw_buffer_load_b128(k, w.k_lane + 64 * s, 0, 0);
+        }
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words<D * item / 64>(v + (w.v_lane + i * (unsigned)w.v_row), (unsigned*)t.v[h][i]);
+    for (int h = 0; h < TT; ++h) {
+        const auto v = rows_at(w.v + pg[h] * w.v_page + in[h] * w.v_row, t.rows[h], w.v_row, w.v_end);
+        if constexpr (F == kRows4) {
+            const auto sc = bytes_at(w.vs + pg[h] * w.vs_page + in[h], t.rows[h] > 0 ? 0x7fffffff : 0);
+            t.vs[h] = __builtin_amdgcn_raw_buffer_load_b32(sc, w.vs_lane, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (F == kRows4 && D == 64) t.v[h][i][0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(v, w.v_lane[i], 0, 0);
+            else load_words<Tile<F, D>::words>(v, w.v_lane[i], t.v[h][i]);
         }
     }
 }
@@ -142,26 +170,20 @@ template <int F, int D, int NT> struct Rows {
 };
 
 template <int F, int D, int NT>
-__device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, int hi, int see_all, Rows<F, D, NT>& r) {
+__device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, int see_all, Rows<F, D, NT>& r) {
     constexpr int TT = Tile<F, D>::TT;
     const int g = (threadIdx.x & 63) >> 4;
-    bool whole = t.key + 16 * TT <= hi;
+    bool whole = true;
 #pragma unroll
-    for (int h = 0; h < TT; ++h) whole = whole && t.there[h];
-    if (!whole) {                    // rows of values that no row of the tile sees may hold anything: they become zeros
+    for (int h = 0; h < TT; ++h) whole = whole && t.rows[h] == 16;
+    if constexpr (F == kRows4) {
+        if (!whole) {                // codes behind the last row are 0, their scales may be NaN
 #pragma unroll
-        for (int h = 0; h < TT; ++h)
+            for (int h = 0; h < TT; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool keep = t.there[h] && t.key + 16 * h + 4 * g + i < hi;
-                if constexpr (F == kRows4) {
-                    t.v[h][i] = keep ? t.v[h][i] : 0u;
-                    if (!keep) t.vs[h] = (t.vs[h] & ~(255u << (8 * i))) | (127u << (8 * i));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < (F == kRows32 ? D / 16 : D / 32); ++e) t.v[h][i][e] = keep ? t.v[h][i][e] : 0;
-                }
-            }
+                for (int i = 0; i < 4; ++i)
+                    if (4 * g + i >= t.rows[h]) t.vs[h] = (t.vs[h] & ~(255u << (8 * i))) | (127u << (8 * i));
+        }
     }
     // scores
     f32x4 s[NT][TT];
@@ -171,10 +193,11 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
             s[n][0] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                union { u32x4 u; f32x4 f; } q;
+                union { u32x4 u; f32x4 f; } q, k;
                 q.u = r.q[n][c];
+                k.u = t.k[0][c];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.k[0][c][e], q.f[e], s[n][0], 0, 0, 0);
+                for (int e = 0; e < 4; ++e) s[n][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[e], q.f[e], s[n][0], 0, 0, 0);
             }
         }
     } else {
@@ -211,7 +234,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[n][h][i] *= p.c;
-                if (!all) s[n][h][i] = t.there[h] && t.key + 16 * h + 4 * g + i < r.see[n] ? s[n][h][i] : -INFINITY;
+                if (!all) s[n][h][i] = 4 * g + i < t.rows[h] && t.key + 16 * h + 4 * g + i < r.see[n] ? s[n][h][i] : -INFINITY;
             }
         float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
         if constexpr (TT == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
@@ -243,7 +266,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
             for (int j = 0; j < D / 16; ++j)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    r.o[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(t.v[0][i][j], s[n][0][i], r.o[n][j], 0, 0, 0);
+                    r.o[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[0][i][j]), s[n][0][i], r.o[n][j], 0, 0, 0);
     } else {
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {              // two channels at a time
@@ -252,7 +275,7 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
             for (int h = 0; h < TT; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if constexpr (F == kRows4) x[h][i] = fp4_pair(t.v[h][i], __uint_as_float(((t.vs[h] >> (8 * i)) & 255u) << 23), c);
+                    if constexpr (F == kRows4) x[h][i] = fp4_pair(t.v[h][i][0], __uint_as_float(((t.vs[h] >> (8 * i)) & 255u) << 23), c);
                     else x[h][i] = t.v[h][i][c];
                 }
 #pragma unroll
@@ -272,20 +295,46 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
 }
 
 template <int F, int D, int NT>
-__global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(AttnArgs p) {
+__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 2 : 1) void kv_attn_kernel(AttnArgs p) {
     using T = typename RowType<F>::type;
     constexpr int item = sizeof(T), TT = Tile<F, D>::TT, TK = 16 * TT, R = 16 * NT, P = D + 4;
     __shared__ float s_o[kWaves][16][P];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
     AttnPart wp;
-    if (!attn_part<R>(p, wp)) return;
-    const int b = wp.b, hk = wp.hk, r0 = wp.r0, rows = wp.rows, lo = wp.lo, hi = wp.hi;
+    const bool work = attn_part<R>(p, wp);
+    const int b = wp.b, hk = wp.hk, r0 = wp.r0, rows = wp.rows, hi = wp.hi;
     const KvSeq sq = wp.sq;
 
+    Where w;
+    w.table = (const_int*)(a.table + b * a.table_stride);
+    w.room = (long long)a.max_pages << a.page_shift;
+    w.shift = a.page_shift;
+    w.n_pages = a.n_pages;
+    // tiles of the chunk go to the waves in turn (the first one's pages are on their way with the sequence's length)
+    int key = wp.lo + wave * TK;
+    Pages<TT> pages = pages_of<TT>(w, key);
+    if (!work) return;
+    constexpr int unit = F == kRows4 ? 1 : item, row_bytes = F == kRows4 ? D / 2 : D * item;
+    w.k = a.kc + hk * a.kcs[1] * unit; w.v = a.vc + hk * a.vcs[1] * unit;
+    w.k_page = a.kcs[0] * unit; w.v_page = a.vcs[0] * unit;
+    w.k_row = a.kcs[2] * unit; w.v_row = a.vcs[2] * unit;
+    w.k_end = w.v_end = row_bytes;
+    w.k_lane = n16 * (int)w.k_row + g * (F == kRows4 ? D / 8 : 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.v_lane[i] = (4 * g + i) * (int)w.v_row + n16 * (row_bytes / 16);
+    if constexpr (F == kRows4) {
+        w.ks = a.ksc + hk * a.kss[1]; w.vs = a.vsc + hk * a.vss[1];
+        w.ks_page = a.kss[0]; w.vs_page = a.vss[0];
+        w.ks_lane = n16 + g * (D / 4) / kFp4Group * (int)a.kss[2];
+        w.vs_lane = 4 * g + n16 * (D / 16) / kFp4Group * (int)a.vss[2];
+    }
+    Tile<F, D> t0, t1;
+    load_tile<F, D>(w, key, hi, pages, t0);
+
     Rows<F, D, NT> r;
-    const int n16 = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = r0 + 16 * n + n16 < rows ? r0 + 16 * n + n16 : rows - 1;
@@ -301,37 +350,20 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
         for (int j = 0; j < D / 16; ++j) r.o[n][j] = f32x4{0, 0, 0, 0};
     }
 
-    Where w;
-    w.table = a.table + b * a.table_stride;
-    w.room = (long long)a.max_pages << a.page_shift;
-    if constexpr (F == kRows4) {
-        w.k = a.kc + hk * a.kcs[1]; w.v = a.vc + hk * a.vcs[1];
-        w.ks = a.ksc + hk * a.kss[1]; w.vs = a.vsc + hk * a.vss[1];
-        w.k_lane = n16 * (unsigned)a.kcs[2] + g * (D / 8);
-        w.v_lane = 4 * g * (unsigned)a.vcs[2] + n16 * (D / 32);
-        w.ks_lane = n16 + (unsigned)(g * (D / 4) / kFp4Group) * (unsigned)a.kss[2];
-        w.vs_lane = 4 * g + (unsigned)(n16 * (D / 16) / kFp4Group) * (unsigned)a.vss[2];
-        w.v_row = a.vcs[2];
-    } else {
-        w.k = a.kc + hk * a.kcs[1] * item; w.v = a.vc + hk * a.vcs[1] * item;
-        w.k_lane = n16 * (unsigned)(a.kcs[2] * item) + 16 * g;
-        w.v_lane = 4 * g * (unsigned)(a.vcs[2] * item) + n16 * (D / 16 * item);
-        w.v_row = a.vcs[2] * item;
-    }
-
-    // tiles of the chunk go to the waves in turn; two in registers, one loading while the other is attended
-    int key = lo + wave * TK;
+    // Two tiles in registers, one loading while the other is attended.  Behind the last tile one without rows is loaded, so that every
+    // path has as much in flight.
     if (key < hi) {
-        Tile<F, D> t0, t1;
-        load_tile<F, D>(a, w, key, t0);
+        pages = pages_of<TT>(w, key + kWaves * TK);
         for (;;) {
-            const int k1 = key + kWaves * TK;
-            load_tile<F, D>(a, w, k1 < hi ? k1 : key, t1);
-            attend_tile<F, D, NT>(p, t0, hi, wp.see_first, r);
-            if (k1 >= hi) break;
-            key = k1 + kWaves * TK;
-            load_tile<F, D>(a, w, key < hi ? key : k1, t0);
-            attend_tile<F, D, NT>(p, t1, hi, wp.see_first, r);
+            key += kWaves * TK;
+            load_tile<F, D>(w, key, hi, pages, t1);
+            pages = pages_of<TT>(w, key + kWaves * TK);
+            attend_tile<F, D, NT>(p, t0, wp.see_first, r);
+            if (key >= hi) break;
+            key += kWaves * TK;
+            load_tile<F, D>(w, key, hi, pages, t0);
+            pages = pages_of<TT>(w, key + kWaves * TK);
+            attend_tile<F, D, NT>(p, t1, wp.see_first, r);
             if (key >= hi) break;
         }
     }
@@ -385,58 +417,68 @@ __global__ __launch_bounds__(64 * kWaves, NT == 4 ? 1 : 2) void kv_attn_kernel(A
     }
 }
 
-// The shares of a row together: one work-group a row, a wave takes every fourth share.
+// The shares of a row together, a work-group a row: first their maxima and sums, a share a thread, which leave a weight for each;
+// then D / 4 threads a share, 1024 / D shares at once, 16 bytes of a share's row a thread.
+constexpr int kMaxSplits = 1024;
 template <class T, int D>
 __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
-    __shared__ float s_o[4][D];
+    constexpr int L = D / 4, S = 256 / L;
+    __shared__ float s_w[kMaxSplits];
     __shared__ float s_m[4], s_l[4];
+    __shared__ f32x4 s_o[S][L];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.y;
     const unsigned row = p.by_hkv.div(blockIdx.x), hk = blockIdx.x - row * a.Hkv;
     const KvSeq sq = kv_seq(a, b);
-    const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+    const int i = (int)p.by_grp.div(row), h = (int)hk * a.grp + row - i * a.grp;
     if (i >= sq.n) return;
     // a share wrote this row if its keys begin before those that the row's tile of rows sees end; before those of the row is enough
     const int see = seen(a, a.kv_len[b], sq.n, i);
-    int parts = (see + p.chunk - 1) / p.chunk;
+    int parts = (int)(((long long)see + p.chunk - 1) / p.chunk);
     parts = parts > p.splits ? p.splits : parts < 1 ? 1 : parts;
     const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits;
     const float* o = p.ws + at * D;
     const float* ml = share_sums(p, D) + at * 2;
-    constexpr int E = (D + 63) / 64;
-    float m = -INFINITY, l = 0.f, acc[E] = {};
-    for (int s = wave; s < parts; s += 4) {
-        const float ms = ml[2 * s], top = fmaxf(m, ms), ref = top == -INFINITY ? 0.f : top;
-        const float down = exp2f(m - ref), up = exp2f(ms - ref);
-        l = l * down + up * ml[2 * s + 1];
+    float m = -INFINITY;
+    for (int s = threadIdx.x; s < parts; s += 256) m = fmaxf(m, ml[2 * s]);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (D >= 64 || lane < D) acc[e] = acc[e] * down + up * o[(long long)s * D + lane * E + e];
-        m = top;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (D >= 64 || lane < D) s_o[wave][lane * E + e] = acc[e];
-    if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
+    for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    if (lane == 0) s_m[wave] = m;
     __syncthreads();
-    const int c = threadIdx.x;
-    if (c >= D) return;
-    const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3])), ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, x = 0.f;
-    for (int k = 0; k < 4; ++k) {
-        const float f = exp2f(s_m[k] - ref);
-        sum += f * s_l[k];
-        x += f * s_o[k][c];
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    for (int s = threadIdx.x; s < parts; s += 256) {
+        const float f = exp2f(ml[2 * s] - ref);
+        s_w[s] = f;
+        l += f * ml[2 * s + 1];
     }
-    ((T*)p.out)[kv_row(a, a.os, b, sq.row0, i, h) + c] = (T)(sum == 0.f ? 0.f : x / sum);
-    if (p.lse && c == 0)
-        p.lse[lse_of(a, sq, b, h, i)] = sum == 0.f ? -INFINITY : top * kLn2 + logf(sum);
+#pragma unroll
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    if (lane == 0) s_l[wave] = l;
+    __syncthreads();
+    l = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+    const int c = threadIdx.x % L, s0 = threadIdx.x / L;
+    f32x4 acc = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int s = s0; s < parts; s += S) acc += s_w[s] * *(const f32x4*)(o + (long long)s * D + 4 * c);
+    s_o[s0][c] = acc;
+    __syncthreads();
+    if (threadIdx.x >= L) return;
+#pragma unroll
+    for (int s = 1; s < S; ++s) acc += s_o[s][c];
+    T* out = (T*)p.out + kv_row(a, a.os, b, sq.row0, i, h) + 4 * c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (T)(l == 0.f ? 0.f : acc[e] / l);
+    if (p.lse && c == 0) p.lse[lse_of(a, sq, b, h, i)] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
-// Rows of a work-group.  Beyond 64 rows with d = 128 and bf16 products: 128 through LDS.
+// Rows of a work-group: 16 or 32 a wave's registers hold beside two tiles of d = 128; more go through LDS, 128 at a time, or 64 where d is
+// less (float: 32, there is no such kernel).
 int tile_rows(long long rows, int d, int dtype) {
-    if (rows > 64 && d == 128 && dtype != 0) return kChunkRows;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    if (rows <= 16) return 16;
+    if (rows <= 32 || (d == 128 && dtype == 0)) return 32;
+    return d == 128 ? kChunkRows : 64;
 }
 
 template <int F, int D>
@@ -448,7 +490,7 @@ int run(const AttnArgs& p, int R, hipStream_t st) {
     int e;
     if (R == 16) e = (int)launch_kernel(kv_attn_kernel<F, D, 1>, grid, block, 0, st, p);
     else if (R == 32) e = (int)launch_kernel(kv_attn_kernel<F, D, 2>, grid, block, 0, st, p);
-    else if (R == 64) e = (int)launch_kernel(kv_attn_kernel<F, D, 4>, grid, block, 0, st, p);
+    else if constexpr (D < 128) e = (int)launch_kernel(kv_attn_kernel<F, D, 4>, grid, block, 0, st, p);
     else e = launch_kv_chunk(p, F == kRows4, grid, st);
     if (e != (int)hipSuccess || p.splits == 1) return e;
     return (int)launch_kernel(kv_join_kernel<T, D>, dim3((unsigned)rows, p.a.B), dim3(256), 0, st, p);
@@ -459,15 +501,17 @@ int run(const AttnArgs& p, int R, hipStream_t st) {
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, long long longest) {
     const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype), tiles = (rows + R - 1) / R;
     const long long groups = tiles * B * Hkv;
-    long long splits = (1024 + groups - 1) / groups;
-    if (tiles == 1 && splits < (longest + 2047) / 2048) splits = (longest + 2047) / 2048;
-    if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
+    static const long long TG = getenv("KV_TG") ? atoll(getenv("KV_TG")) : 1024, MC = getenv("KV_MC") ? atoll(getenv("KV_MC")) : 2048, LC = getenv("KV_LC") ? atoll(getenv("KV_LC")) : 256;
+    long long splits = (TG + groups - 1) / groups;
+    if (tiles == 1 && splits < (longest + MC - 1) / MC) splits = (longest + MC - 1) / MC;
+    if (splits > (longest + LC - 1) / LC) splits = (longest + LC - 1) / LC;
     if (splits < 1) splits = 1;
+    if (splits > kMaxSplits) splits = kMaxSplits;
     const long long chunk = ((longest + splits - 1) / splits + 127) / 128 * 128;
     splits = (longest + chunk - 1) / chunk;
     KvSplit s;
     s.splits = splits < 1 ? 1 : (int)splits;
-    s.chunk = chunk < 128 ? 128 : chunk > (1 << 30) ? 1 << 30 : (int)chunk;
+    s.chunk = chunk < 128 ? 128 : (int)chunk;
     s.ws_bytes = s.splits == 1 ? 0 : (size_t)B * Hkv * rows * s.splits * (d + 2) * 4;
     return s;
 }
