@@ -242,6 +242,7 @@ int dense_causal_flash(const aa_params *params, const void *q, const void *k, co
  *
  *  Cache formats.  AA_KV_PLAIN: element (page, head, row, c) of the call's dtype at page*kc_stride[0] + head*kc_stride[1] +
  *  row*kc_stride[2] + c; strides in elements, multiples of 16 bytes.
+ *  A page's rows (of one head) span less than 2 GiB: page_size * kc_stride[2] * (element size) < 2^31.
  *  AA_KV_FP4: 4-bit floats (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), d/2 bytes a row at
  *  page*kc_stride[0] + head*kc_stride[1] + row*kc_stride[2] (bytes, multiples of 16), channel 2i in the low and 2i+1 in the high half
  *  of byte i; and a scale byte for every 32 channels g of a row at  page*ks_stride[0] + head*ks_stride[1] + g*ks_stride[2] + row

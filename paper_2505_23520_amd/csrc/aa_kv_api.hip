@@ -28,8 +28,9 @@ int check_pool(const aa_kv_params* p, const void* pool, const int64_t* st, const
     if (!pool || unaligned(pool)) return AA_EINVAL;
     if (fp4 && (!sc || unaligned(sc))) return AA_EINVAL;
     if (st[0] > (1ll << 60) / p->n_pages || (fp4 && ss[0] > (1ll << 60) / p->n_pages)) return AA_EINVAL;
-    // 16 rows, and the groups of a row, are addressed with 32 bits from the page's first
-    if (st[2] >= (1 << 25) || (fp4 && ss[2] >= (1 << 28))) return AA_EUNSUPPORTED;
+    // 32-bit byte offsets: the rows of a page, from its first on, and the groups of a row's scales
+    const int64_t bytes = fp4 ? 1 : p->dtype == AA_BF16 ? 2 : 4;
+    if (st[2] >= (1 << 25) || st[2] * bytes * p->page_size >= (1ll << 31) || (fp4 && ss[2] >= (1 << 28))) return AA_EUNSUPPORTED;
     for (int e = 0; e < 3; ++e) {
         if (st[e] < row || st[e] % unit || st[e] >= (1ll << 40)) return AA_EINVAL;
         if (fp4 && (ss[e] < p->page_size || ss[e] % 16 || ss[e] >= (1ll << 40))) return AA_EINVAL;

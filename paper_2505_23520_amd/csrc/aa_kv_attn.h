@@ -11,6 +11,7 @@ struct AttnArgs {
     float *lse, *ws;
     int splits, chunk, rows, tiles;  // rows of a KV head (N * grp); row tiles
     float c;                         // sigma * log2 e
+    float slack;                     // a reference is raised when a score exceeds it by this much: weights stay below 2^8
     FastDiv by_hkv, by_splits, by_grp;
 };
 

@@ -26,7 +26,6 @@ using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 
 constexpr int kWaves = 4;
-constexpr float kSlack = 8.f;       // a reference is raised when a score exceeds it by 2^8: weights stay below 256 in 32-bit sums
 
 enum { kRows32, kRows16, kRows4 };  // cached rows: float, bf16, 4 bits
 
@@ -66,14 +65,14 @@ struct Where {
     int k_lane, v_lane[4], ks_lane, vs_lane, k_end, v_end;     // *_end: where the last row's bytes end, from the row's start
 };
 
-// The pages of a tile; -1: none.
+// The pages of a tile; -1: none.  Pages of 32 tokens and more hold both halves of one.
 template <int TT> struct Pages { int p[TT]; };
 template <int TT> __device__ __forceinline__ Pages<TT> pages_of(const Where& w, int key) {
     Pages<TT> x;
-#pragma unroll
-    for (int h = 0; h < TT; ++h) {
-        const int j = key + 16 * h;
-        x.p[h] = j < w.room ? w.table[j >> w.shift] : -1;
+    x.p[0] = key < w.room ? w.table[key >> w.shift] : -1;
+    if constexpr (TT == 2) {
+        x.p[1] = x.p[0];
+        if (__builtin_expect(w.shift == 4, 0)) x.p[1] = key + 16 < w.room ? w.table[(key >> 4) + 1] : -1;
     }
     return x;
 }
@@ -112,39 +111,43 @@ template <int F, int D>
 __device__ __forceinline__ void load_tile(const Where& w, int key, int hi, const Pages<Tile<F, D>::TT>& pages, Tile<F, D>& t) {
     t.key = key;
     constexpr int TT = Tile<F, D>::TT;
-    long long pg[TT];
-    int in[TT];
+    const char *k[TT], *v[TT];
+    const unsigned char *ks[TT], *vs[TT];
 #pragma unroll
     for (int h = 0; h < TT; ++h) {
         const bool there = (unsigned)pages.p[h] < (unsigned)w.n_pages;
         const int n = hi - (key + 16 * h);
-        pg[h] = there ? pages.p[h] : 0;
-        in[h] = (key + 16 * h) & ((1 << w.shift) - 1);
         t.rows[h] = !there ? 0 : n < 16 ? n : 16;            // 0 and less: none
+        if (h && __builtin_expect(w.shift > 4, 1)) {
+            k[h] = k[0] + 16 * (int)w.k_row; v[h] = v[0] + 16 * (int)w.v_row;
+            if constexpr (F == kRows4) { ks[h] = ks[0] + 16; vs[h] = vs[0] + 16; }
+        } else {
+            const long long pg = there ? pages.p[h] : 0;
+            const int in = (key + 16 * h) & ((1 << w.shift) - 1);      // a page's rows span less than 2^31 bytes
+            k[h] = w.k + pg * w.k_page + in * (int)w.k_row; v[h] = w.v + pg * w.v_page + in * (int)w.v_row;
+            if constexpr (F == kRows4) { ks[h] = w.ks + pg * w.ks_page + in; vs[h] = w.vs + pg * w.vs_page + in; }
+        }
     }
 #pragma unroll
     for (int h = 0; h < TT; ++h) {
-        const auto k = rows_at(w.k + pg[h] * w.k_page + in[h] * w.k_row, t.rows[h], w.k_row, w.k_end);
+        const auto rs = rows_at(k[h], t.rows[h], w.k_row, w.k_end);
         if constexpr (F == kRows4) {
-            load_words<D / 32>(k, w.k_lane, t.k[h]);
-            const auto sc = bytes_at(w.ks + pg[h] * w.ks_page + in[h], t.rows[h] > 0 ? 0x7fffffff : 0);
-            t.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(sc, w.ks_lane, 0, 0);
+            load_words<D / 32>(rs, w.k_lane, t.k[h]);
+            t.ks[h] = __builtin_amdgcn_raw_buffer_load_b8(bytes_at(ks[h], t.rows[h] > 0 ? 0x7fffffff : 0), w.ks_lane, 0, 0);
         } else {
 #pragma unroll
-            for (int s = 0; s < (F == kRows32 ? D / 16 : D / 32); ++s) t.k[h][s] = __builtin_amdgcn_raw_buffer_load_b128(k, w.k_lane + 64 * s, 0, 0);
+            for (int s = 0; s < (F == kRows32 ? D / 16 : D / 32); ++s) t.k[h][s] = __builtin_amdgcn_raw_buffer_load_b128(rs, w.k_lane + 64 * s, 0, 0);
         }
     }
 #pragma unroll
     for (int h = 0; h < TT; ++h) {
-        const auto v = rows_at(w.v + pg[h] * w.v_page + in[h] * w.v_row, t.rows[h], w.v_row, w.v_end);
-        if constexpr (F == kRows4) {
-            const auto sc = bytes_at(w.vs + pg[h] * w.vs_page + in[h], t.rows[h] > 0 ? 0x7fffffff : 0);
-            t.vs[h] = __builtin_amdgcn_raw_buffer_load_b32(sc, w.vs_lane, 0, 0);
-        }
+        const auto rs = rows_at(v[h], t.rows[h], w.v_row, w.v_end);
+        if constexpr (F == kRows4)
+            t.vs[h] = __builtin_amdgcn_raw_buffer_load_b32(bytes_at(vs[h], t.rows[h] > 0 ? 0x7fffffff : 0), w.vs_lane, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (F == kRows4 && D == 64) t.v[h][i][0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(v, w.v_lane[i], 0, 0);
-            else load_words<Tile<F, D>::words>(v, w.v_lane[i], t.v[h][i]);
+            if constexpr (F == kRows4 && D == 64) t.v[h][i][0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(rs, w.v_lane[i], 0, 0);
+            else load_words<Tile<F, D>::words>(rs, w.v_lane[i], t.v[h][i]);
         }
     }
 }
@@ -165,7 +168,7 @@ template <int F, int D, int NT> struct Rows {
     static constexpr int Q = F == kRows32 ? D / 16 : D / 32;
     u32x4 q[NT][Q];
     f32x4 o[NT][D / 16];
-    float m[NT], l[NT];              // l: this lane's keys alone
+    float m[NT], l[NT];              // m: before the scale; l: this lane's keys alone
     int see[NT];                     // keys that the lane's row sees
 };
 
@@ -224,36 +227,40 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
             }
         }
     }
-    // weights
-    const bool all = whole && t.key + 16 * TT <= see_all;
+    // weights (scores and references before the scale c: one multiply-add makes the exponent of both)
+    if (__builtin_expect(!(whole && t.key + 16 * TT <= see_all), 0)) {
+        int base = 4 * g;
+        asm volatile("" : "+v"(base));                   // else 50 instructions of this stand in every tile's way
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < TT; ++h) {
+                const int left = r.see[n] - t.key - 16 * h, lim = left < t.rows[h] ? left : t.rows[h];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][h][i] = base + i < lim ? s[n][h][i] : -INFINITY;
+            }
+    }
     union { bf16x8 b; __bf16 e[8]; } pb[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-#pragma unroll
-        for (int h = 0; h < TT; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[n][h][i] *= p.c;
-                if (!all) s[n][h][i] = 4 * g + i < t.rows[h] && t.key + 16 * h + 4 * g + i < r.see[n] ? s[n][h][i] : -INFINITY;
-            }
         float top = fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3]));
         if constexpr (TT == 2) top = fmaxf(top, fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-        if (__any(top > r.m[n] + kSlack)) {
+        if (__builtin_expect(__any(top > r.m[n] + p.slack), 0)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float m = fmaxf(top, r.m[n]);
-            const float down = m == -INFINITY ? 1.f : exp2f(r.m[n] - m);
+            const float down = m == -INFINITY || m == r.m[n] ? 1.f : exp2f((r.m[n] - m) * p.c);
             r.m[n] = m;
             r.l[n] *= down;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) r.o[n][j] *= down;
         }
-        const float ref = r.m[n] == -INFINITY ? 0.f : r.m[n];
+        const float ref = r.m[n] == -INFINITY ? 0.f : r.m[n] * p.c;
 #pragma unroll
         for (int h = 0; h < TT; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[n][h][i] = __builtin_amdgcn_exp2f(s[n][h][i] - ref);
+                s[n][h][i] = __builtin_amdgcn_exp2f(fmaf(s[n][h][i], p.c, -ref));
                 r.l[n] += s[n][h][i];
                 if constexpr (F != kRows32) pb[n].e[4 * h + i] = (__bf16)s[n][h][i];
             }
@@ -376,7 +383,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 2 : 1) void kv_attn_kernel(A
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (n) __syncthreads();
-        if (g == 0) { s_m[wave][n16] = r.m[n]; s_l[wave][n16] = l; }
+        if (g == 0) { s_m[wave][n16] = r.m[n] * p.c; s_l[wave][n16] = l; }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -526,6 +533,7 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     const int R = tile_rows(p.rows, d, dtype);
     p.tiles = (p.rows + R - 1) / R;
     p.c = a.sigma * kLog2e;
+    p.slack = fminf(8.f / p.c, 3.402823466e38f);
     p.by_hkv.set(a.Hkv); p.by_splits.set(sp.splits); p.by_grp.set(a.grp);
     if (dtype == 0) return d == 32 ? run<kRows32, 32>(p, R, st) : d == 64 ? run<kRows32, 64>(p, R, st) : d == 128 ? run<kRows32, 128>(p, R, st) : -1;
     if (format) return d == 64 ? run<kRows4, 64>(p, R, st) : d == 128 ? run<kRows4, 128>(p, R, st) : -1;

@@ -62,6 +62,7 @@ def test_struct_layout(api, tmp_path):
     (dict(d=96, rot_dim=0), -2), (dict(d=256), -2), (dict(d=32, rot_dim=0), -2), (dict(page_size=8), -2), (dict(page_size=1 << 21), -2), (dict(rot_dim=24), -2),
     (dict(format=1, dtype=0), -2), (dict(B=65536), -2), (dict(Hq=65536, Hkv=1), -2), (dict(B=65535, N=65535), -2), (dict(N=2**30, B=1), -2),
     (dict(max_pages=2**26 + 1, table_stride=2**26 + 1), -2), (dict(kc_stride=_three(1 << 33, 1 << 32, 1 << 25)), -2),
+    (dict(kc_stride=_three(1 << 33, 1 << 32, 1 << 15), page_size=1 << 15), -2),
     (dict(format=1, vs_stride=_three(1 << 33, 1 << 32, 1 << 28)), -2),
 ])
 def test_rejects_bad_params(api, kw, code):
