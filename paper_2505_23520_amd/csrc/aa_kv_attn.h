@@ -1,6 +1,7 @@
 // What the kernels of kv_attn share.
 #pragma once
 #include "aa_kv.h"
+#include "aa_kv_deal.h"
 
 namespace aa {
 
@@ -9,10 +10,12 @@ struct AttnArgs {
     const void* q;
     void* out;
     float *lse, *ws;
-    int splits, chunk, rows, tiles;  // rows of a KV head (N * grp); row tiles
+    int rows, tiles;                 // most rows of a KV head and sequence (N * grp), their row tiles
+    int groups;                      // registers: work-groups that the line of units is dealt to
+    int splits, chunk;               // LDS: work-groups of a row tile, keys of each (the last one's: what is left)
     float c;                         // sigma * log2 e
     float slack;                     // a reference is raised when a score exceeds it by this much: weights stay below 2^8
-    FastDiv by_hkv, by_splits, by_grp;
+    FastDiv by_hkv, by_splits, by_grp, by_groups;
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

@@ -22,6 +22,7 @@ namespace {
 using u32x2 = __attribute__((ext_vector_type(2))) unsigned;
 using u32x4 = __attribute__((ext_vector_type(4))) unsigned;
 using f32x4 = __attribute__((ext_vector_type(4))) float;
+using f32x2 = __attribute__((ext_vector_type(2))) float;
 using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 
@@ -53,6 +54,9 @@ template <int D> struct Tile<kRows32, D> {
     unsigned v[TT][4][words];
     int key, rows[TT];
 };
+
+// Waves of a SIMD that a kernel's registers allow, and so work-groups of a CU.
+template <int F, int D, int NT> constexpr int kOccupancy = NT == 1 ? (D == 128 ? (F == kRows4 ? 3 : 2) : D == 64 ? 3 : 4) : NT == 2 && D < 128 ? 2 : 1;
 
 // What a wave needs to find a tile: its sequence's pages, the pools from its head on, and a lane's place in 16 keys (bytes).
 struct Where {
@@ -301,31 +305,122 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
     }
 }
 
+// A sequence as a work-group's stretch meets it.
+struct Part { int b, len, units, tiles; KvSeq sq; };
+template <int R> __device__ __forceinline__ Part part_of(const AttnArgs& p, int b) {
+    Part x;
+    x.b = b;
+    x.sq = kv_seq(p.a, b);
+    x.len = p.a.kv_len[b];
+    x.units = deal_units(seen(p.a, x.len, x.sq.n, x.sq.n - 1), x.sq.n);
+    x.tiles = (x.sq.n * p.a.grp + R - 1) / R;
+    return x;
+}
+
+// Sums of the lanes up to each lane: within 16, then over the rows of 16 before.
+__device__ __forceinline__ unsigned wave_scan(unsigned x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// The line of units (see aa_kv_deal.h) as a wave works it out alone, 64 sequences at a time: units of one KV head, and the sequence that
+// holds unit `at` of a head with the units before it.
+template <int R> struct Line {
+    const AttnArgs& p;
+    Part y;                                                  // the lane's sequence
+    unsigned x, upto;                                        // its units; with those before in the same 64
+    __device__ __forceinline__ Line(const AttnArgs& args) : p(args) {}
+    __device__ __forceinline__ void load(int first) {
+        const int b = first + (threadIdx.x & 63);
+        x = 0;
+        if (b < p.a.B) {
+            y = part_of<R>(p, b);
+            x = (unsigned)y.units * y.tiles;
+        }
+        upto = wave_scan(x);
+    }
+    __device__ __forceinline__ unsigned units() {
+        unsigned sum = 0;
+        for (int first = 0; first < p.a.B; first += 64) {
+            load(first);
+            sum += __builtin_amdgcn_readlane(upto, 63);
+        }
+        return sum;
+    }
+    // after units()
+    __device__ __forceinline__ Part find(unsigned at, unsigned* before) {
+        unsigned base = 0;
+        for (int first = 0; first < p.a.B; first += 64) {
+            if (p.a.B > 64) load(first);
+            const unsigned long long after = __ballot(base + upto > at);
+            if (after) {
+                const int l = __ffsll(after) - 1;
+                *before = base + __builtin_amdgcn_readlane(upto - x, l);
+                Part s;
+                s.b = first + l;
+                s.len = __builtin_amdgcn_readlane(y.len, l);
+                s.units = __builtin_amdgcn_readlane(y.units, l);
+                s.tiles = __builtin_amdgcn_readlane(y.tiles, l);
+                s.sq.n = __builtin_amdgcn_readlane(y.sq.n, l);
+                s.sq.row0 = (long long)(unsigned)__builtin_amdgcn_readlane((int)y.sq.row0, l);     // rows are counted in 31 bits
+                return s;
+            }
+            base += __builtin_amdgcn_readlane(upto, 63);
+        }
+        return part_of<R>(p, 0);                             // not reached: `at` is below units()
+    }
+};
+
+__device__ __forceinline__ Deal deal_of(const AttnArgs& p, unsigned total) {
+    Deal d;
+    d.each = p.by_groups.div(total);
+    d.more = total - d.each * p.groups;
+    return d;
+}
+
+// What the joining kernel is told by the work-group that ends inside a tile which it has begun (the first of those that share it).
+struct Shared { int b, hk, r0, count; };
+__device__ __forceinline__ Shared* shared_tiles(const AttnArgs& p, int R, int D) { return (Shared*)(p.ws + 2ll * p.groups * R * (D + 2)); }
+
 template <int F, int D, int NT>
-__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 2 : 1) void kv_attn_kernel(AttnArgs p) {
+__global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_kernel(AttnArgs p) {
     using T = typename RowType<F>::type;
     constexpr int item = sizeof(T), TT = Tile<F, D>::TT, TK = 16 * TT, R = 16 * NT, P = D + 4;
+    static_assert(kUnitKeys % (kWaves * TK) == 0, "a unit is whole rounds of the waves");
     __shared__ float s_o[kWaves][16][P];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g = lane >> 4;
-    AttnPart wp;
-    const bool work = attn_part<R>(p, wp);
-    const int b = wp.b, hk = wp.hk, r0 = wp.r0, rows = wp.rows, hi = wp.hi;
-    const KvSeq sq = wp.sq;
+    // this work-group's stretch, and where it begins
+    unsigned head_units, before = 0;
+    Part s = part_of<R>(p, 0);
+    Line<R> line(p);
+    if (a.B == 1) head_units = (unsigned)s.units * s.tiles;
+    else head_units = line.units();
+    Shared* const told = p.ws && a.B > 1 ? shared_tiles(p, R, D) + blockIdx.x : nullptr;
+    if (told && threadIdx.x == 0) told->count = 0;
+    const unsigned total = head_units * a.Hkv;
+    const Deal deal = deal_of(p, total);
+    unsigned at = deal_start(deal, blockIdx.x);
+    const unsigned end = deal_start(deal, blockIdx.x + 1);
+    if (at >= end) return;
+    int hk = (int)(at / head_units);
+    const unsigned in_head = at - hk * head_units;
+    if (a.B > 1) s = line.find(in_head, &before);
+    int tile_no = p.tiles == 1 ? 0 : (int)((in_head - before) / s.units);
+    int t = (int)(in_head - before) - tile_no * s.units;
 
     Where w;
-    w.table = (const_int*)(a.table + b * a.table_stride);
     w.room = (long long)a.max_pages << a.page_shift;
     w.shift = a.page_shift;
     w.n_pages = a.n_pages;
-    // tiles of the chunk go to the waves in turn (the first one's pages are on their way with the sequence's length)
-    int key = wp.lo + wave * TK;
-    Pages<TT> pages = pages_of<TT>(w, key);
-    if (!work) return;
     constexpr int unit = F == kRows4 ? 1 : item, row_bytes = F == kRows4 ? D / 2 : D * item;
-    w.k = a.kc + hk * a.kcs[1] * unit; w.v = a.vc + hk * a.vcs[1] * unit;
     w.k_page = a.kcs[0] * unit; w.v_page = a.vcs[0] * unit;
     w.k_row = a.kcs[2] * unit; w.v_row = a.vcs[2] * unit;
     w.k_end = w.v_end = row_bytes;
@@ -333,151 +428,231 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 2 : 1) void kv_attn_kernel(A
 #pragma unroll
     for (int i = 0; i < 4; ++i) w.v_lane[i] = (4 * g + i) * (int)w.v_row + n16 * (row_bytes / 16);
     if constexpr (F == kRows4) {
-        w.ks = a.ksc + hk * a.kss[1]; w.vs = a.vsc + hk * a.vss[1];
         w.ks_page = a.kss[0]; w.vs_page = a.vss[0];
         w.ks_lane = n16 + g * (D / 4) / kFp4Group * (int)a.kss[2];
         w.vs_lane = 4 * g + n16 * (D / 16) / kFp4Group * (int)a.vss[2];
     }
-    Tile<F, D> t0, t1;
-    load_tile<F, D>(w, key, hi, pages, t0);
 
-    Rows<F, D, NT> r;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = r0 + 16 * n + n16 < rows ? r0 + 16 * n + n16 : rows - 1;
-        const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
-        r.see[n] = seen(a, wp.len, sq.n, i);
-        r.m[n] = -INFINITY;
-        r.l[n] = 0.f;
-        const char* q = (const char*)p.q + kv_row(a, a.qs, b, sq.row0, i, h) * item;
-#pragma unroll
-        for (int c = 0; c < Rows<F, D, NT>::Q; ++c)
-            r.q[n][c] = *(const u32x4*)(q + (F == kRows4 ? (D / 2) * g + 16 * c : 64 * c + 16 * g));
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) r.o[n][j] = f32x4{0, 0, 0, 0};
-    }
-
-    // Two tiles in registers, one loading while the other is attended.  Behind the last tile one without rows is loaded, so that every
-    // path has as much in flight.
-    if (key < hi) {
+    for (;;) {                                           // over the row tiles that the stretch touches
+        const int stop = s.units - t < (int)(end - at) ? s.units : t + (int)(end - at);
+        const int r0 = tile_no * R, rows = s.sq.n * a.grp, last = r0 + R < rows ? r0 + R - 1 : rows - 1;
+        const int see_first = seen(a, s.len, s.sq.n, (int)p.by_grp.div(r0)), see_last = seen(a, s.len, s.sq.n, (int)p.by_grp.div(last));
+        const int hi = stop * kUnitKeys < see_last ? stop * kUnitKeys : see_last;
+        w.table = (const_int*)(a.table + s.b * a.table_stride);
+        w.k = a.kc + hk * a.kcs[1] * unit; w.v = a.vc + hk * a.vcs[1] * unit;
+        if constexpr (F == kRows4) { w.ks = a.ksc + hk * a.kss[1]; w.vs = a.vsc + hk * a.vss[1]; }
+        // tiles of keys go to the waves in turn
+        int key = t * kUnitKeys + wave * TK;
+        Pages<TT> pages = pages_of<TT>(w, key);
+        Tile<F, D> t0, t1;
+        load_tile<F, D>(w, key, hi, pages, t0);
         pages = pages_of<TT>(w, key + kWaves * TK);
-        for (;;) {
-            key += kWaves * TK;
-            load_tile<F, D>(w, key, hi, pages, t1);
-            pages = pages_of<TT>(w, key + kWaves * TK);
-            attend_tile<F, D, NT>(p, t0, wp.see_first, r);
-            if (key >= hi) break;
-            key += kWaves * TK;
-            load_tile<F, D>(w, key, hi, pages, t0);
-            pages = pages_of<TT>(w, key + kWaves * TK);
-            attend_tile<F, D, NT>(p, t1, wp.see_first, r);
-            if (key >= hi) break;
-        }
-    }
 
-    // the waves' rows together, 16 at a time
-    const int x = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * (D / 16);
+        Rows<F, D, NT> r;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        float l = r.l[n];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (n) __syncthreads();
-        if (g == 0) { s_m[wave][n16] = r.m[n] * p.c; s_l[wave][n16] = l; }
+        for (int n = 0; n < NT; ++n) {
+            const int row = r0 + 16 * n + n16 < rows ? r0 + 16 * n + n16 : rows - 1;
+            const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+            r.see[n] = seen(a, s.len, s.sq.n, i);
+            r.m[n] = -INFINITY;
+            r.l[n] = 0.f;
+            const char* q = (const char*)p.q + kv_row(a, a.qs, s.b, s.sq.row0, i, h) * item;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int c = 0; c < Rows<F, D, NT>::Q; ++c)
+                r.q[n][c] = *(const u32x4*)(q + (F == kRows4 ? (D / 2) * g + 16 * c : 64 * c + 16 * g));
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) s_o[wave][n16][(D / 16) * (4 * g + i) + j] = r.o[n][j][i];
-        __syncthreads();
-        const int row = r0 + 16 * n + x;
-        if (row >= rows) continue;
-        float m = -INFINITY, sum = 0.f, acc[D / 16] = {};
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) m = fmaxf(m, s_m[k][x]);
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-            const float f = exp2f(s_m[k][x] - ref);
-            sum += f * s_l[k][x];
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) acc[j] += f * s_o[k][x][c0 + j];
+            for (int j = 0; j < D / 16; ++j) r.o[n][j] = f32x4{0, 0, 0, 0};
         }
-        const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
-        if (p.splits > 1) {
-            const long long at = share_of(p, wp, row);
-            float* o = p.ws + at * D + c0;
-#pragma unroll
-            for (int j = 0; j < D / 16; ++j) o[j] = acc[j];
-            if (c0 == 0) {
-                float* ml = share_sums(p, D) + at * 2;
-                ml[0] = m; ml[1] = sum;
+
+        // Two tiles in registers, one loading while the other is attended.  Behind the last one a tile without rows is loaded, so that every
+        // path has as much in flight.  (Three or four tiles for 4 bits: slower, 131 / 133 / 153 us for 64 sequences, 0.5 M keys.)
+        if (key < hi) {
+            for (;;) {
+                key += kWaves * TK;
+                load_tile<F, D>(w, key, hi, pages, t1);
+                pages = pages_of<TT>(w, key + kWaves * TK);
+                attend_tile<F, D, NT>(p, t0, see_first, r);
+                if (key >= hi) break;
+                key += kWaves * TK;
+                load_tile<F, D>(w, key, hi, pages, t0);
+                pages = pages_of<TT>(w, key + kWaves * TK);
+                attend_tile<F, D, NT>(p, t1, see_first, r);
+                if (key >= hi) break;
             }
-        } else {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            T* o = (T*)p.out + kv_row(a, a.os, b, sq.row0, i, h) + c0;
+        }
+
+        // the waves' rows together, 16 at a time
+        const int x = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * (D / 16);
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) o[j] = (T)(acc[j] * inv);
-            if (p.lse && c0 == 0)
-                p.lse[lse_of(a, sq, b, h, i)] =
-                    sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
+        for (int n = 0; n < NT; ++n) {
+            float l = r.l[n];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            __syncthreads();                             // the last rows have been read
+            if (g == 0) { s_m[wave][n16] = r.m[n] * p.c; s_l[wave][n16] = l; }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) s_o[wave][n16][(D / 16) * (4 * g + i) + j] = r.o[n][j][i];
+            __syncthreads();
+            const int row = r0 + 16 * n + x;
+            if (row >= rows) continue;
+            float m = -INFINITY, sum = 0.f, acc[D / 16] = {};
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) m = fmaxf(m, s_m[k][x]);
+            const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                const float f = exp2f(s_m[k][x] - ref);
+                sum += f * s_l[k][x];
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) acc[j] += f * s_o[k][x][c0 + j];
+            }
+            if (t > 0 || stop < s.units) {
+                const long long place = (long long)deal_place(blockIdx.x, t) * R + 16 * n + x;
+                float* o = p.ws + place * D + c0;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[j] = acc[j];
+                if (c0 == 0) {
+                    float* ml = p.ws + 2ll * p.groups * R * D + place * 2;
+                    ml[0] = m; ml[1] = sum;
+                }
+            } else {
+                const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                T* o = (T*)p.out + kv_row(a, a.os, s.b, s.sq.row0, i, h) + c0;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[j] = (T)(acc[j] * inv);
+                if (p.lse && c0 == 0) p.lse[lse_of(a, s.sq, s.b, h, i)] = sum == 0.f ? -INFINITY : m * kLn2 + logf(sum);
+            }
+        }
+
+        if (told && t == 0 && stop < s.units && threadIdx.x == 0) 
+            *told = Shared{s.b, hk, r0, (int)(deal_group(deal, at + s.units - 1) - blockIdx.x) + 1};
+
+        // the next row tile
+        at += stop - t;
+        if (at >= end) return;
+        t = 0;
+        if (++tile_no == s.tiles) {
+            tile_no = 0;
+            int b = s.b;
+            do {                                         // (ends: units are left)
+                if (++b == a.B) { b = 0; ++hk; }
+                s = part_of<R>(p, b);
+            } while (s.units == 0);
         }
     }
 }
 
-// The shares of a row together, a work-group a row: first their maxima and sums, a share a thread, which leave a weight for each;
-// then D / 4 threads a share, 1024 / D shares at once, 16 bytes of a share's row a thread.
-constexpr int kMaxSplits = 1024;
-template <class T, int D>
-__global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
-    constexpr int L = D / 4, S = 256 / L;
-    __shared__ float s_w[kMaxSplits];
-    __shared__ float s_m[4], s_l[4];
-    __shared__ f32x4 s_o[S][L];
-    const KvArgs& a = p.a;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.y;
-    const unsigned row = p.by_hkv.div(blockIdx.x), hk = blockIdx.x - row * a.Hkv;
-    const KvSeq sq = kv_seq(a, b);
-    const int i = (int)p.by_grp.div(row), h = (int)hk * a.grp + row - i * a.grp;
-    if (i >= sq.n) return;
-    // a share wrote this row if its keys begin before those that the row's tile of rows sees end; before those of the row is enough
-    const int see = seen(a, a.kv_len[b], sq.n, i);
-    int parts = (int)(((long long)see + p.chunk - 1) / p.chunk);
-    parts = parts > p.splits ? p.splits : parts < 1 ? 1 : parts;
-    const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits;
-    const float* o = p.ws + at * D;
-    const float* ml = share_sums(p, D) + at * 2;
-    float m = -INFINITY;
-    for (int s = threadIdx.x; s < parts; s += 256) m = fmaxf(m, ml[2 * s]);
+// The shares of a row together, a wave a row or (TEAM = 4) a work-group a row: first their maxima and sums, a share a lane, which leave a
+// weight for each in LDS; then D / 4 lanes a share, 16 bytes of its row each, 256 / D shares a wave at once and eight times as many on
+// their way.
+// place(s): where share s stands; o, ml: the first place's values, and maximum and sum.
+// mine: maximum and sum of share `lane`, requested ahead (of a share beyond count: anything).
+constexpr int kMaxShares = 1024;
+template <class T, int D, int TEAM, class Place>
+__device__ __forceinline__ void join_row(const AttnArgs& p, int count, const float* o, const float* ml, Place place, f32x2 mine,
+                                         float* weights, f32x4* part, T* out, float* lse) {
+    constexpr int L = D / 4, S = 64 / L;
+    const int lane = threadIdx.x & 63, wave = TEAM == 1 ? 0 : threadIdx.x >> 6;
+    if (lane >= count) mine = f32x2{-INFINITY, 0.f};
+    float m = mine[0];
+    for (int s = lane + 64; s < count; s += 64) m = fmaxf(m, ml[2 * place(s)]);
 #pragma unroll
     for (int x = 32; x; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    if (lane == 0) s_m[wave] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
     const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int s = threadIdx.x; s < parts; s += 256) {
-        const float f = exp2f(ml[2 * s] - ref);
-        s_w[s] = f;
-        l += f * ml[2 * s + 1];
+    float l = exp2f(mine[0] - ref) * mine[1];
+    weights[lane] = exp2f(mine[0] - ref);                    // every wave its own: LDS keeps a wave's order
+    for (int s = lane + 64; s < count; s += 64) {
+        const float f = exp2f(ml[2 * place(s)] - ref);
+        weights[s] = f;
+        l += f * ml[2 * place(s) + 1];
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    if (lane == 0) s_l[wave] = l;
-    __syncthreads();
-    l = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-    const int c = threadIdx.x % L, s0 = threadIdx.x / L;
+    const int c = lane % L;
     f32x4 acc = {0, 0, 0, 0};
-#pragma unroll 8
-    for (int s = s0; s < parts; s += S) acc += s_w[s] * *(const f32x4*)(o + (long long)s * D + 4 * c);
-    s_o[s0][c] = acc;
-    __syncthreads();
-    if (threadIdx.x >= L) return;
+    for (int s0 = wave * S + lane / L; s0 < count; s0 += 8 * TEAM * S) {     // eight requests at a time, also of the last ones (again, with weight 0)
+        f32x4 v[8];
 #pragma unroll
-    for (int s = 1; s < S; ++s) acc += s_o[s][c];
-    T* out = (T*)p.out + kv_row(a, a.os, b, sq.row0, i, h) + 4 * c;
+        for (int k = 0; k < 8; ++k) v[k] = *(const f32x4*)(o + place(s0 + k * TEAM * S < count ? s0 + k * TEAM * S : count - 1) * D + 4 * c);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = (T)(l == 0.f ? 0.f : acc[e] / l);
-    if (p.lse && c == 0) p.lse[lse_of(a, sq, b, h, i)] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+        for (int k = 0; k < 8; ++k) acc += (s0 + k * TEAM * S < count ? weights[s0 + k * TEAM * S] : 0.f) * v[k];
+    }
+#pragma unroll
+    for (int x = L; x < 64; x *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
+    if constexpr (TEAM > 1) {
+        if (lane < L) part[wave * L + c] = acc;
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int k = 1; k < TEAM; ++k) acc += part[k * L + c];
+    }
+    if (lane >= L) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[4 * c + e] = (T)(l == 0.f ? 0.f : acc[e] / l);
+    if (lse && c == 0) *lse = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+}
+
+// The chunk kernel's shares, which stand row by row: a work-group for four rows of a KV head.
+template <class T, int D>
+__global__ __launch_bounds__(256) void kv_join_rows_kernel(AttnArgs p) {
+    __shared__ float s_w[4][kMaxShares];
+    const KvArgs& a = p.a;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int b = blockIdx.y, four = (int)p.by_hkv.div(blockIdx.x), hk = (int)blockIdx.x - four * a.Hkv, row = 4 * four + wave;
+    const KvSeq sq = kv_seq(a, b);
+    const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+    if (i >= sq.n) return;
+    // a share wrote this row if its keys begin before those that the row's tile of rows sees end; before those of the row is enough
+    int parts = (int)(((long long)seen(a, a.kv_len[b], sq.n, i) + p.chunk - 1) / p.chunk);
+    parts = parts > p.splits ? p.splits : parts < 1 ? 1 : parts;
+    const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits;
+    const float* ml = share_sums(p, D);
+    join_row<T, D, 1>(p, parts, p.ws, ml, [=](int s) { return at + s; }, *(const f32x2*)(ml + 2 * (at + (lane < parts ? lane : 0))), s_w[wave],
+                      nullptr, (T*)p.out + kv_row(a, a.os, b, sq.row0, i, h), p.lse ? p.lse + lse_of(a, sq, b, h, i) : nullptr);
+}
+
+// kv_attn_kernel's shares of several sequences: its work-groups tell which tiles are shared; a work-group for four rows of each.
+template <class T, int D, int R>
+__global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
+    __shared__ float s_w[4][kMaxShares];
+    const KvArgs& a = p.a;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int group = blockIdx.x, r = 4 * blockIdx.y + wave;
+    auto place = [=](int s) { return (long long)deal_place(group + s, s) * R + r; };
+    const float* ml = p.ws + 2ll * p.groups * R * D;
+    const f32x2 mine = *(const f32x2*)(ml + 2 * place(group + lane < p.groups ? lane : 0));      // some place's: on its way with what is told
+    const Shared told = shared_tiles(p, R, D)[group];
+    if (!told.count) return;
+    const KvSeq sq = kv_seq(a, told.b);
+    const int row = told.r0 + r, i = (int)p.by_grp.div(row), h = told.hk * a.grp + row - i * a.grp;
+    if (r >= R || i >= sq.n) return;
+    join_row<T, D, 1>(p, told.count, p.ws, ml, place, mine, s_w[wave], nullptr, (T*)p.out + kv_row(a, a.os, told.b, sq.row0, i, h),
+                      p.lse ? p.lse + lse_of(a, sq, told.b, h, i) : nullptr);
+}
+
+// Of one sequence: where a tile's units are dealt to is known without being told, and a tile has many shares; a work-group a row.
+template <class T, int D, int R>
+__global__ __launch_bounds__(256) void kv_join_one_kernel(AttnArgs p) {
+    __shared__ float s_w[4][kMaxShares];
+    __shared__ f32x4 s_o[D];
+    const KvArgs& a = p.a;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int row = (int)p.by_hkv.div(blockIdx.x), hk = (int)blockIdx.x - row * a.Hkv, i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
+    const Part s = part_of<R>(p, 0);
+    if (i >= s.sq.n) return;
+    const Deal deal = deal_of(p, (unsigned)s.units * s.tiles * a.Hkv);
+    const unsigned first = ((unsigned)hk * s.tiles + row / R) * s.units;
+    const int group = (int)deal_group(deal, first), count = (int)deal_group(deal, first + s.units - 1) - group + 1;
+    if (count == 1) return;                                  // finished where it was computed
+    auto place = [=](int k) { return (long long)deal_place(group + k, k) * R + row % R; };
+    const float* ml = p.ws + 2ll * p.groups * R * D;
+    join_row<T, D, 4>(p, count, p.ws, ml, place, *(const f32x2*)(ml + 2 * place(lane < count ? lane : 0)), s_w[wave], s_o,
+                      (T*)p.out + kv_row(a, a.os, 0, s.sq.row0, i, h), p.lse ? p.lse + lse_of(a, s.sq, 0, h, i) : nullptr);
 }
 
 // Rows of a work-group: 16 or 32 a wave's registers hold beside two tiles of d = 128; more go through LDS, 128 at a time, or 64 where d is
@@ -488,38 +663,60 @@ int tile_rows(long long rows, int d, int dtype) {
     return d == 128 ? kChunkRows : 64;
 }
 
+template <int F, int D, int NT>
+int run_registers(const AttnArgs& p, hipStream_t st) {
+    using T = typename RowType<F>::type;
+    int e = (int)launch_kernel(kv_attn_kernel<F, D, NT>, dim3(p.groups), dim3(64 * kWaves), 0, st, p);
+    if (e != (int)hipSuccess || !p.ws) return e;
+    if (p.a.B == 1) return (int)launch_kernel(kv_join_one_kernel<T, D, 16 * NT>, dim3((unsigned)p.a.Hkv * p.rows), dim3(256), 0, st, p);
+    return (int)launch_kernel(kv_join_kernel<T, D, 16 * NT>, dim3(p.groups, ((p.rows < 16 * NT ? p.rows : 16 * NT) + 3) / 4), dim3(256), 0, st, p);
+}
+
 template <int F, int D>
 int run(const AttnArgs& p, int R, hipStream_t st) {
     using T = typename RowType<F>::type;
-    const long long x = (long long)p.a.Hkv * p.tiles * p.splits, rows = (long long)p.a.Hkv * p.rows;
-    if (x > 0x7fffffffll || (p.splits > 1 && rows > 0x7fffffffll)) return -1;
-    const dim3 grid((unsigned)x, p.a.B), block(64 * kWaves);
-    int e;
-    if (R == 16) e = (int)launch_kernel(kv_attn_kernel<F, D, 1>, grid, block, 0, st, p);
-    else if (R == 32) e = (int)launch_kernel(kv_attn_kernel<F, D, 2>, grid, block, 0, st, p);
-    else if constexpr (D < 128) e = (int)launch_kernel(kv_attn_kernel<F, D, 4>, grid, block, 0, st, p);
-    else e = launch_kv_chunk(p, F == kRows4, grid, st);
+    if ((long long)p.a.Hkv * p.rows > 0x7fffffffll) return -1;
+    if (R == 16) return run_registers<F, D, 1>(p, st);
+    if (R == 32) return run_registers<F, D, 2>(p, st);
+    if constexpr (D < 128) return run_registers<F, D, 4>(p, st);
+    const long long x = (long long)p.a.Hkv * p.tiles * p.splits;
+    if (x > 0x7fffffffll) return -1;
+    const int e = launch_kv_chunk(p, F == kRows4, dim3((unsigned)x, p.a.B), st);
     if (e != (int)hipSuccess || p.splits == 1) return e;
-    return (int)launch_kernel(kv_join_kernel<T, D>, dim3((unsigned)rows, p.a.B), dim3(256), 0, st, p);
+    return (int)launch_kernel(kv_join_rows_kernel<T, D>, dim3((unsigned)p.a.Hkv * ((p.rows + 3) / 4), p.a.B), dim3(256), 0, st, p);
 }
+
+template <int F, int D> int occupancy(int R) { return R == 16 ? kOccupancy<F, D, 1> : R == 32 ? kOccupancy<F, D, 2> : kOccupancy<F, D, 4>; }
+
+constexpr int kCUs = 256;
 
 }  // namespace
 
-KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, long long longest) {
+KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room) {
     const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype), tiles = (rows + R - 1) / R;
-    const long long groups = tiles * B * Hkv;
+    const long long items = tiles * B * Hkv;
+    KvSplit s = {0, 1, 0, 0};
+    if (R < kChunkRows) {
+        // as many work-groups as run at once, or as there are units
+        const int o = dtype == 0 ? (d == 32 ? occupancy<kRows32, 32>(R) : d == 64 ? occupancy<kRows32, 64>(R) : occupancy<kRows32, 128>(R))
+                    : format ? (d == 64 ? occupancy<kRows4, 64>(R) : occupancy<kRows4, 128>(R))
+                             : d == 64 ? occupancy<kRows16, 64>(R) : occupancy<kRows16, 128>(R);
+        static const int GM = getenv("KV_GM") ? atoi(getenv("KV_GM")) : 100;
+        const long long units = deal_units((int)longest, 1), most = kCUs * o * GM / 100;
+        s.groups = (int)(units * items < most ? units * items : most);
+        if (room > kUnitKeys) s.ws_bytes = 2ull * s.groups * R * (d + 2) * 4 + s.groups * sizeof(Shared);
+        return s;
+    }
     static const long long TG = getenv("KV_TG") ? atoll(getenv("KV_TG")) : 1024, MC = getenv("KV_MC") ? atoll(getenv("KV_MC")) : 2048, LC = getenv("KV_LC") ? atoll(getenv("KV_LC")) : 256;
-    long long splits = (TG + groups - 1) / groups;
+    long long splits = (TG + items - 1) / items;
     if (tiles == 1 && splits < (longest + MC - 1) / MC) splits = (longest + MC - 1) / MC;
     if (splits > (longest + LC - 1) / LC) splits = (longest + LC - 1) / LC;
     if (splits < 1) splits = 1;
-    if (splits > kMaxSplits) splits = kMaxSplits;
+    if (splits > kMaxShares) splits = kMaxShares;
     const long long chunk = ((longest + splits - 1) / splits + 127) / 128 * 128;
-    splits = (longest + chunk - 1) / chunk;
-    KvSplit s;
-    s.splits = splits < 1 ? 1 : (int)splits;
-    s.chunk = chunk < 128 ? 128 : (int)chunk;
-    s.ws_bytes = s.splits == 1 ? 0 : (size_t)B * Hkv * rows * s.splits * (d + 2) * 4;
+    s.splits = (int)((longest + chunk - 1) / chunk);
+    s.chunk = (int)chunk;
+    if (s.splits > 1) s.ws_bytes = (size_t)B * Hkv * rows * s.splits * (d + 2) * 4;
     return s;
 }
 
@@ -527,14 +724,15 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
                    hipStream_t st) {
     AttnArgs p;
     p.a = a;
-    p.q = q; p.out = out; p.lse = lse; p.ws = ws;
-    p.splits = sp.splits; p.chunk = sp.chunk;
+    p.q = q; p.out = out; p.lse = lse;
+    p.ws = sp.ws_bytes ? ws : nullptr;
+    p.groups = sp.groups; p.splits = sp.splits; p.chunk = sp.chunk;
     p.rows = a.N * a.grp;
     const int R = tile_rows(p.rows, d, dtype);
     p.tiles = (p.rows + R - 1) / R;
     p.c = a.sigma * kLog2e;
     p.slack = fminf(8.f / p.c, 3.402823466e38f);
-    p.by_hkv.set(a.Hkv); p.by_splits.set(sp.splits); p.by_grp.set(a.grp);
+    p.by_hkv.set(a.Hkv); p.by_splits.set(sp.splits); p.by_grp.set(a.grp); p.by_groups.set(sp.groups ? sp.groups : 1);
     if (dtype == 0) return d == 32 ? run<kRows32, 32>(p, R, st) : d == 64 ? run<kRows32, 64>(p, R, st) : d == 128 ? run<kRows32, 128>(p, R, st) : -1;
     if (format) return d == 64 ? run<kRows4, 64>(p, R, st) : d == 128 ? run<kRows4, 128>(p, R, st) : -1;
     return d == 64 ? run<kRows16, 64>(p, R, st) : d == 128 ? run<kRows16, 128>(p, R, st) : -1;
