@@ -13,7 +13,6 @@
 //                keys 4g .. 4g+3 of each half of the tile, and the sum over keys may run in that order too.  The left operand wants 8 keys of
 //                one channel in a lane; a lane loads D/16 channels of each of its keys and two byte permutations turn four bf16 values.
 // A lane's rows of S^T, O^T, m and the sum are all row lane % 16, so nothing crosses lanes unless a reference is raised.
-#include <stdlib.h>
 #include "aa_kv_attn.h"
 
 namespace aa {
@@ -701,17 +700,17 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
         const int o = dtype == 0 ? (d == 32 ? occupancy<kRows32, 32>(R) : d == 64 ? occupancy<kRows32, 64>(R) : occupancy<kRows32, 128>(R))
                     : format ? (d == 64 ? occupancy<kRows4, 64>(R) : occupancy<kRows4, 128>(R))
                              : d == 64 ? occupancy<kRows16, 64>(R) : occupancy<kRows16, 128>(R);
-        static const int GM = getenv("KV_GM") ? atoi(getenv("KV_GM")) : 100;
-        const long long units = deal_units((int)longest, 1), most = kCUs * o * GM / 100;
-        s.groups = (int)(units * items < most ? units * items : most);
+        const long long units = items * deal_units((int)longest, 1);
+        s.groups = (int)(units < kCUs * o ? units : kCUs * o);
         if (room > kUnitKeys) s.ws_bytes = 2ull * s.groups * R * (d + 2) * 4 + s.groups * sizeof(Shared);
         return s;
     }
-    static const long long TG = getenv("KV_TG") ? atoll(getenv("KV_TG")) : 1024, MC = getenv("KV_MC") ? atoll(getenv("KV_MC")) : 2048, LC = getenv("KV_LC") ? atoll(getenv("KV_LC")) : 256;
-    long long splits = (TG + items - 1) / items;
-    if (tiles == 1 && splits < (longest + MC - 1) / MC) splits = (longest + MC - 1) / MC;
-    if (splits > (longest + LC - 1) / LC) splits = (longest + LC - 1) / LC;
-    if (splits < 1) splits = 1;
+    // Row tiles through LDS: all tiles of a KV head begin their keys together, which is what lets an XCD's L2 serve them (dealt evenly like
+    // the others, 2048 and 1000 new tokens over 30011 and 8192 took 1148 us instead of 996).  Keys are split until there are as
+    // many work-groups as run at once, three a CU, or shares of 256 keys.  32 heads, 1024 and 403 new tokens over 16384 and 5003 in 4
+    // bits, work-groups wanted 512 / 768 / 2048: 529 / 369 / 489 us; 100 over 4000 in bf16: 26.2 / 26.0 / 37.
+    long long splits = (kCUs * 3 + items - 1) / items;
+    if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
     if (splits > kMaxShares) splits = kMaxShares;
     const long long chunk = ((longest + splits - 1) / splits + 127) / 128 * 128;
     s.splits = (int)((longest + chunk - 1) / chunk);

@@ -35,9 +35,9 @@ template <bool FP4>
 __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     __shared__ __attribute__((aligned(16))) char Ks0[KBYTES], Ks1[KBYTES], Vs0[VBYTES];
     const KvArgs& a = p.a;
-    const int lane = threadIdx.x & 63;
+    int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 31, hf = lane >> 5;
+    int n = lane & 31, hf = lane >> 5;
     AttnPart w;
     if (!attn_part<kChunkRows>(p, w)) return;
     __builtin_amdgcn_s_setprio(2);                   // against the softmax of the SIMD's other waves
@@ -61,39 +61,48 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     const char* const k0 = a.kc + w.hk * a.kcs[1] * (FP4 ? 1 : 2);
     const char* const v0 = a.vc + w.hk * a.vcs[1] * (FP4 ? 1 : 2);
     const unsigned kstb = (unsigned)a.kcs[2] * (FP4 ? 1 : 2), vstb = (unsigned)a.vcs[2] * (FP4 ? 1 : 2);
-    const unsigned klane = FP4 ? (lane >> 2) * kstb + 16 * (lane & 3) : (lane >> 4) * kstb + 16 * (lane & 15);
-    const unsigned vlane = FP4 ? (lane >> 2) * vstb + 16 * (lane & 3) : (lane >> 4) * vstb + 16 * (lane & 15);
     auto base_of = [&](const char* x0, const long long* st, int j, int page) -> const char* {
         return x0 + ((page < 0 ? 0 : page) * st[0] + (j & ((1 << a.page_shift) - 1)) * st[2]) * (FP4 ? 1 : 2);
     };
-    auto rows_load = [&](const char* base, unsigned stb, unsigned at, char* dst, int pitch) {
+    auto rows_load = [&](const char* base, unsigned stb, char* dst, int pitch) {
+        const int ln = counted_lane();
+        const unsigned at = (ln >> 4) * stb + 16 * (ln & 15);
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(15u * stb + 2u * D), 0x00020000);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(dst + (4 * wave + i) * pitch), 16, (int)at, (int)(4u * i * stb), 0, 0);
     };
     struct Codes { u32x4 x; unsigned byte; };
-    auto codes_load = [&](const char* base, unsigned at, const unsigned char* sc, const long long* ss, int j, int page) -> Codes {
+    auto rsrc_of = [&](const void* x) -> __amdgpu_buffer_rsrc_t {        // (scalar, and said to be)
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)x), hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)x >> 32));
+        return __builtin_amdgcn_make_buffer_rsrc((void*)((uintptr_t)hi << 32 | lo), 0, 0x7fffffff, 0x00020000);
+    };
+    auto codes_load = [&](const char* base, unsigned stb, const unsigned char* sc, const long long* ss, int j, int page) -> Codes {
+        const int ln = counted_lane();
         Codes c;
-        c.x = *(const u32x4*)(base + at);
-        c.byte = (sc + w.hk * ss[1] + (page < 0 ? 0 : page) * ss[0] + (j & ((1 << a.page_shift) - 1)))[(lane >> 2) + (unsigned)(lane & 3) * (unsigned)ss[2]];
+        c.x = __builtin_amdgcn_raw_buffer_load_b128(rsrc_of(base), (int)((ln >> 2) * stb + 16 * (ln & 3)), 0, 0);
+        const unsigned char* s = sc + w.hk * ss[1] + (page < 0 ? 0 : page) * ss[0] + (j & ((1 << a.page_shift) - 1));
+        c.byte = __builtin_amdgcn_raw_buffer_load_b8(rsrc_of(s), (ln >> 2) + (ln & 3) * (int)ss[2], 0, 0);
         return c;
     };
     // piece e of lane 4 key + c goes out in step (e - key) % 4, so that 16 lanes write to all banks
     auto codes_store = [&](const Codes& c, char* stage, int pitch) {
-        const int key = lane >> 2;
-        char* dst = stage + (4 * wave + (key >> 2)) * pitch + (key & 3) * 256 + 64 * (lane & 3);
+        const int ln = counted_lane(), key = ln >> 2;
+        char* dst = stage + (4 * wave + (key >> 2)) * pitch + (key & 3) * 256 + 64 * (ln & 3);
         const float scale = __uint_as_float(c.byte << 23);
+        u32x4 x, y;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] = key & 1 ? c.x[(s + 1) & 3] : c.x[s];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) y[s] = key & 2 ? x[(s + 2) & 3] : x[s];         // piece (s + key) % 4
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int e = (s + key) & 3;
-            const unsigned x = e == 0 ? c.x[0] : e == 1 ? c.x[1] : e == 2 ? c.x[2] : c.x[3];
-            union { u32x4 u; bf16x2 b[4]; } y;
-            y.b[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0);
-            y.b[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1);
-            y.b[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2);
-            y.b[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3);
-            *(u32x4*)(dst + 16 * e) = y.u;
+            union { u32x4 u; bf16x2 b[4]; } v;
+            v.b[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y[s], scale, 0);
+            v.b[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y[s], scale, 1);
+            v.b[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y[s], scale, 2);
+            v.b[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(y[s], scale, 3);
+            *(u32x4*)(dst + 16 * ((s + key) & 3)) = v.u;
         }
     };
 
@@ -119,12 +128,12 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     Codes kc, vc;
     if (nT > 0) {
         if constexpr (FP4) {
-            kc = codes_load(base_of(k0, a.kcs, key_of(0), pg), klane, a.ksc, a.kss, key_of(0), pg);
-            vc = codes_load(base_of(v0, a.vcs, key_of(0), pg), vlane, a.vsc, a.vss, key_of(0), pg);
+            kc = codes_load(base_of(k0, a.kcs, key_of(0), pg), kstb, a.ksc, a.kss, key_of(0), pg);
+            vc = codes_load(base_of(v0, a.vcs, key_of(0), pg), vstb, a.vsc, a.vss, key_of(0), pg);
             codes_store(kc, Ks0, KGRP);
             __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0)
         } else {
-            rows_load(base_of(k0, a.kcs, key_of(0), pg), kstb, klane, Ks0, KGRP);
+            rows_load(base_of(k0, a.kcs, key_of(0), pg), kstb, Ks0, KGRP);
         }
     }
     wait_vmem();
@@ -133,7 +142,7 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     auto tile_step = [&](int t, const char* Kcur, char* Knext) __attribute__((always_inline)) {
         const int t0 = w.lo + TK * t, j = key_of(t);
         if constexpr (FP4) codes_store(vc, Vs0, VGRP);
-        else rows_load(base_of(v0, a.vcs, j, pg), vstb, vlane, Vs0, VGRP);
+        else rows_load(base_of(v0, a.vcs, j, pg), vstb, Vs0, VGRP);
         __builtin_amdgcn_sched_barrier(0);
         // the pages of the whole tile, for the masks
         unsigned there = 0;
@@ -178,10 +187,10 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
         // the next K tile (past the end the last one again, into a stage that nobody reads)
         const int u = t + 1 < nT ? t + 1 : t, ju = key_of(u), pu = t + 1 < nT ? pg_next : pg;
         if constexpr (FP4) {
-            kc = codes_load(base_of(k0, a.kcs, ju, pu), klane, a.ksc, a.kss, ju, pu);
-            vc = codes_load(base_of(v0, a.vcs, ju, pu), vlane, a.vsc, a.vss, ju, pu);
+            kc = codes_load(base_of(k0, a.kcs, ju, pu), kstb, a.ksc, a.kss, ju, pu);
+            vc = codes_load(base_of(v0, a.vcs, ju, pu), vstb, a.vsc, a.vss, ju, pu);
         } else {
-            rows_load(base_of(k0, a.kcs, ju, pu), kstb, klane, Knext, KGRP);
+            rows_load(base_of(k0, a.kcs, ju, pu), kstb, Knext, KGRP);
         }
         __builtin_amdgcn_sched_barrier(0);
         // V tile t has landed: the four loads of the next K tile are younger
@@ -232,8 +241,10 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
         if (t + 1 < nT) tile_step(t + 1, Ks1, Ks0);
     }
 
-    // ---- epilogue
+    // ---- epilogue (no lane's value but addresses lives through the loop)
     const float lt = row_sum(l);
+    lane = counted_lane();
+    n = lane & 31; hf = lane >> 5;
     if (rw >= w.rows) return;
     if (p.splits > 1) {
         if (rw + n >= w.rows) return;
@@ -273,8 +284,9 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
             *(intx4*)((unsigned short*)p.out + kv_row(a, a.os, w.b, w.sq.row0, ti, h) + 8 * c) = x;
         }
     }
-    if (p.lse && hf == 0 && rw + n < w.rows)
-        p.lse[lse_of(a, w.sq, w.b, qh, qi)] = lt == 0.f ? -INFINITY : mref * c2 * kLn2 + logf(lt);
+    if (!p.lse || hf || rw + n >= w.rows) return;
+    const int ti = (int)p.by_grp.div(rw + n), th = w.hk * a.grp + rw + n - ti * a.grp;
+    p.lse[lse_of(a, w.sq, w.b, th, ti)] = lt == 0.f ? -INFINITY : mref * c2 * kLn2 + logf(lt);
 }
 
 }  // namespace
