@@ -122,7 +122,6 @@ struct AppendArgs {
     void *q_out, *k_out;
 };
 
-constexpr int kInFlight = 3;                    // rows of a token that a thread loads before it goes on
 enum { kNoPairs, kHalves, kNeighbours };        // which channels are turned together
 
 __device__ __forceinline__ long long uniform(long long x) {
@@ -130,11 +129,13 @@ __device__ __forceinline__ long long uniform(long long x) {
            (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
 }
 
-template <class T, bool FP4, int D, int PAIRS, int TOKENS>
+// TOKENS: of a work-group; TF of them, PASSES rows of each, are on their way in a thread at once.
+template <class T, bool FP4, int D, int PAIRS, int TOKENS, int TF, int PASSES>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
     constexpr int V = kVec<T>, LANES = D / V, ROWS = 256 / LANES, item = sizeof(T);
     using S = typename std::conditional<FP4, double, float>::type;
     __shared__ S s_cs[TOKENS][D / 2][2];
+    __shared__ float s_csf[FP4 ? TOKENS : 1][D / 2][2];              // 4 bits: the queries' own, rounded once
     __shared__ Token s_tok[TOKENS];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -146,7 +147,14 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
         if (lane == 0) s_tok[wave] = t;
         if (PAIRS != kNoPairs && t.i >= 0 && lane < a.rot / 2) {
             const double pos = p.positions ? (double)p.positions[row_first + wave] : (double)t.j;
-            cos_sin<S>(pos * (double)p.inv_freq[lane], &s_cs[wave][lane][0], &s_cs[wave][lane][1]);
+            S c, s;
+            cos_sin<S>(pos * (double)p.inv_freq[lane], &c, &s);
+            s_cs[wave][lane][0] = c;
+            s_cs[wave][lane][1] = s;
+            if (FP4) {
+                s_csf[wave][lane][0] = (float)c;
+                s_csf[wave][lane][1] = (float)s;
+            }
         }
     }
     __syncthreads();
@@ -155,14 +163,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
     const bool turn = PAIRS != kNoPairs && c < a.rot, upper = PAIRS == kHalves && c >= half;
     const int other = !turn ? 0 : PAIRS == kHalves ? (upper ? -half : half) : 0;         // the pair's other chunk
     const int f0 = !turn ? 0 : PAIRS == kNeighbours ? c / 2 : upper ? c - half : c;
-    for (int r0 = threadIdx.x / LANES + ROWS * kInFlight * blockIdx.y; r0 < rows + threadIdx.x / LANES;
-         r0 += ROWS * kInFlight * gridDim.y) {
-        // where a thread's rows lie from the token's on, in bytes
-        bool is_q[kInFlight], is_v[kInFlight], there[kInFlight];
-        long long from[kInFlight], to[kInFlight], pool[kInFlight];
-        int head[kInFlight];
+    for (int r0 = threadIdx.x / LANES + ROWS * PASSES * blockIdx.y; r0 < rows + threadIdx.x / LANES; r0 += ROWS * PASSES * gridDim.y) {
+        // where a thread's rows lie from the token's on
+        bool is_q[PASSES], is_v[PASSES], there[PASSES];
+        long long from[PASSES], to[PASSES], pool[PASSES];
+        int head[PASSES];
 #pragma unroll
-        for (int u = 0; u < kInFlight; ++u) {
+        for (int u = 0; u < PASSES; ++u) {
             const int r = r0 + u * ROWS < rows ? r0 + u * ROWS : rows - 1;
             there[u] = r0 + u * ROWS < rows;
             is_q[u] = r < nq;
@@ -174,80 +181,90 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
             pool[u] = (long long)h * (is_v[u] ? a.vcs[1] : a.kcs[1]) + (FP4 ? c / 2 : c);
         }
 #pragma unroll 1
-        for (int tk = 0; tk < TOKENS; ++tk) {
-            const int i = __builtin_amdgcn_readfirstlane(s_tok[tk].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk].b);
-            if (i < 0) continue;
-            const int page = __builtin_amdgcn_readfirstlane(s_tok[tk].page), in = __builtin_amdgcn_readfirstlane(s_tok[tk].in);
-            const long long row0 = uniform(s_tok[tk].row0);
-            const T* q = (const T*)p.q + kv_row(a, a.qs, b, row0, i, 0);
-            const T* k = (const T*)p.k + kv_row(a, a.ks, b, row0, i, 0);
-            const T* v = (const T*)p.v + kv_row(a, a.vs, b, row0, i, 0);
-            u32x4 x[kInFlight], z[kInFlight];
+        for (int tk0 = 0; tk0 < TOKENS; tk0 += TF) {
+            u32x4 x[TF][PASSES], z[TF][PASSES];
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                const T* src = (is_q[u] ? q : is_v[u] ? v : k) + from[u];
-                x[u] = *(const u32x4*)src;
-                if (PAIRS == kHalves) z[u] = *(const u32x4*)(src + other);
-            }
-            float cs[V], sn[V];
-            if (PAIRS != kNoPairs && !FP4) {
+            for (int f = 0; f < TF; ++f) {
+                const int i = __builtin_amdgcn_readfirstlane(s_tok[tk0 + f].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk0 + f].b);
+                if (i < 0) continue;
+                const long long row0 = uniform(s_tok[tk0 + f].row0);
+                const T* q = (const T*)p.q + kv_row(a, a.qs, b, row0, i, 0);
+                const T* k = (const T*)p.k + kv_row(a, a.ks, b, row0, i, 0);
+                const T* v = (const T*)p.v + kv_row(a, a.vs, b, row0, i, 0);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const int f = f0 + (PAIRS == kNeighbours ? e / 2 : e);
-                    cs[e] = s_cs[tk][f][0];
-                    sn[e] = s_cs[tk][f][1];
-                    if (PAIRS == kNeighbours ? !(e & 1) : !upper) sn[e] = -sn[e];
+                for (int u = 0; u < PASSES; ++u) {
+                    const T* src = (is_q[u] ? q : is_v[u] ? v : k) + from[u];
+                    x[f][u] = *(const u32x4*)src;
+                    if (PAIRS == kHalves) z[f][u] = *(const u32x4*)(src + other);
                 }
             }
-            T* qo = (T*)p.q_out + kv_row(a, a.os, b, row0, i, 0);
-            T* ko = (T*)p.k_out + kv_row(a, a.kos, b, row0, i, 0);
-            char* kc = a.kc + (page * a.kcs[0] + in * a.kcs[2]) * (FP4 ? 1 : item);
-            char* vc = a.vc + (page * a.vcs[0] + in * a.vcs[2]) * (FP4 ? 1 : item);
 #pragma unroll
-            for (int u = 0; u < kInFlight; ++u) {
-                float y[V], m[V];
-                unpack<T>(x[u], y);
-                if (PAIRS == kHalves) {
-                    unpack<T>(z[u], m);
-                } else {
+            for (int f = 0; f < TF; ++f) {
+                const int tk = tk0 + f;
+                const int i = __builtin_amdgcn_readfirstlane(s_tok[tk].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk].b);
+                if (i < 0) continue;
+                const int page = __builtin_amdgcn_readfirstlane(s_tok[tk].page), in = __builtin_amdgcn_readfirstlane(s_tok[tk].in);
+                const long long row0 = uniform(s_tok[tk].row0);
+                float cs[V], sn[V];
+                if (PAIRS != kNoPairs) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) m[e] = y[e ^ 1];
+                    for (int e = 0; e < V; ++e) {
+                        const int g = f0 + (PAIRS == kNeighbours ? e / 2 : e);
+                        if constexpr (FP4) { cs[e] = s_csf[tk][g][0]; sn[e] = s_csf[tk][g][1]; }
+                        else { cs[e] = s_cs[tk][g][0]; sn[e] = s_cs[tk][g][1]; }
+                        if (PAIRS == kNeighbours ? !(e & 1) : !upper) sn[e] = -sn[e];
+                    }
                 }
-                const bool turned = turn && !is_v[u];
-                u32x4 w = x[u];
-                if constexpr (!FP4) {
+                T* qo = (T*)p.q_out + kv_row(a, a.os, b, row0, i, 0);
+                T* ko = (T*)p.k_out + kv_row(a, a.kos, b, row0, i, 0);
+                char* kc = a.kc + (page * a.kcs[0] + in * a.kcs[2]) * (FP4 ? 1 : item);
+                char* vc = a.vc + (page * a.vcs[0] + in * a.vcs[2]) * (FP4 ? 1 : item);
+#pragma unroll
+                for (int u = 0; u < PASSES; ++u) {
+                    float y[V], m[V];
+                    unpack<T>(x[f][u], y);
+                    if (PAIRS == kHalves) {
+                        unpack<T>(z[f][u], m);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) m[e] = y[e ^ 1];
+                    }
+                    const bool turned = turn && !is_v[u];
+                    u32x4 w = x[f][u];
+                    float t[V];
                     if (PAIRS != kNoPairs) {
 #pragma unroll
-                        for (int e = 0; e < V; ++e) y[e] = fmaf(m[e], sn[e], y[e] * cs[e]);
-                        const u32x4 r = pack<T>(y);
+                        for (int e = 0; e < V; ++e) t[e] = fmaf(m[e], sn[e], y[e] * cs[e]);
+                        const u32x4 r = pack<T>(t);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) w[e] = turned ? r[e] : w[e];
                     }
-                } else if (turned) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const int f = f0 + (PAIRS == kNeighbours ? e / 2 : e);
-                        const S c64 = s_cs[tk][f][0], s64 = (PAIRS == kNeighbours ? !(e & 1) : !upper) ? -s_cs[tk][f][1] : s_cs[tk][f][1];
-                        y[e] = is_q[u] ? fmaf(m[e], (float)s64, y[e] * (float)c64) : to_odd(fma((double)m[e], s64, y[e] * c64));
+                    if (!there[u]) continue;
+                    if (is_q[u]) {
+                        *(u32x4*)(qo + to[u]) = w;
+                        continue;
                     }
-                    w = pack<T>(y);
-                }
-                if (!there[u]) continue;
-                if (is_q[u]) {
-                    *(u32x4*)(qo + to[u]) = w;
-                    continue;
-                }
-                if (p.k_out && !is_v[u]) *(u32x4*)(ko + to[u]) = w;
-                if (page < 0) continue;
-                if constexpr (!FP4) {
-                    *(u32x4*)((is_v[u] ? vc : kc) + pool[u] * item) = w;
-                } else {
-                    int byte;
-                    *(unsigned*)((is_v[u] ? vc : kc) + pool[u]) = to_fp4(y, &byte);
-                    if (c % kFp4Group) continue;
-                    unsigned char* sc = is_v[u] ? a.vsc + page * a.vss[0] + head[u] * a.vss[1] + c / kFp4Group * a.vss[2]
-                                                : a.ksc + page * a.kss[0] + head[u] * a.kss[1] + c / kFp4Group * a.kss[2];
-                    sc[in] = (unsigned char)byte;
+                    if (p.k_out && !is_v[u]) *(u32x4*)(ko + to[u]) = w;
+                    if (page < 0) continue;
+                    if constexpr (!FP4) {
+                        *(u32x4*)((is_v[u] ? vc : kc) + pool[u] * item) = w;
+                    } else {
+                        // codes are taken from the 64-bit values: of two neighbours in 32 bits one may be on another code's side
+                        if (turned) {
+#pragma unroll
+                            for (int e = 0; e < V; ++e) {
+                                const int g = f0 + (PAIRS == kNeighbours ? e / 2 : e);
+                                const double s64 = (PAIRS == kNeighbours ? !(e & 1) : !upper) ? -s_cs[tk][g][1] : s_cs[tk][g][1];
+                                y[e] = to_odd(fma((double)m[e], s64, y[e] * (double)s_cs[tk][g][0]));
+                            }
+                        }
+                        int byte;
+                        *(unsigned*)((is_v[u] ? vc : kc) + pool[u]) = to_fp4(y, &byte);
+                        if (c % kFp4Group) continue;
+                        unsigned char* sc = is_v[u] ? a.vsc + page * a.vss[0] + head[u] * a.vss[1] + c / kFp4Group * a.vss[2]
+                                                    : a.ksc + page * a.kss[0] + head[u] * a.kss[1] + c / kFp4Group * a.kss[2];
+                        sc[in] = (unsigned char)byte;
+                    }
                 }
             }
         }
@@ -313,14 +330,14 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a, T* k_out, T* v_o
 
 template <class T, bool FP4, int D, int PAIRS>
 int run_pairs(const AppendArgs& p, hipStream_t st) {
-    constexpr int PASS = 256 / (D / kVec<T>) * kInFlight;          // rows of a token in one pass of a work-group
+    constexpr int ROWS = 256 / (D / kVec<T>);                      // rows of a token that a work-group takes at once
     const int rows = (p.q_out ? p.a.Hq : 0) + (p.k ? 2 * p.a.Hkv : 0);
-    // Few tokens: a work-group a pass of a token's rows, so that none waits for a second one.
-    if (p.a.total < 1024) {
-        const int passes = (rows + PASS - 1) / PASS;
-        return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1>, dim3((unsigned)p.a.total, passes < 64 ? passes : 64), dim3(256), 0, st, p);
-    }
-    return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4>, dim3((unsigned)((p.a.total + 3) / 4)), dim3(256), 0, st, p);
+    const dim3 block(256), few((unsigned)p.a.total, (rows + 3 * ROWS - 1) / (3 * ROWS)), many((unsigned)((p.a.total + 3) / 4));
+    // Few tokens: a work-group for three passes over a token's rows, so that none waits for another.
+    if (p.a.total < 1024) return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1, 1, 3>, dim3(few.x, few.y < 64 ? few.y : 64), block, 0, st, p);
+    // Few rows: those of four tokens on their way instead of three passes of one.
+    if (rows <= ROWS) return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 4, 1>, many, block, 0, st, p);
+    return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 1, 3>, many, block, 0, st, p);
 }
 template <class T, bool FP4, int D>
 int run_append(const AppendArgs& p, hipStream_t st) {
