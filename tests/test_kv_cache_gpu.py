@@ -90,6 +90,40 @@ def test_attn_packed(api, dtype, fp4, d, causal):
     _check_attn(api, cache, q, new, packed=True, causal=causal)
 
 
+@pytest.mark.parametrize("dtype,fp4,d", [(BF, False, 128), (BF, True, 128), (BF, False, 64), (F32, False, 64)])
+@pytest.mark.parametrize("new", [1, 3, 20])
+def test_attn_many_sequences(api, dtype, fp4, d, new):
+    """More sequences than a wave has lanes, of very different lengths, empty ones among them: packed, some without new tokens."""
+    lens = [(i * i * 977) % 1500 if i % 7 else (0, 1, 128, 129)[i // 7 % 4] for i in range(150)] + [5000]
+    news = [new if i % 5 else (i // 5) % (new + 1) for i in range(150)] + [new]
+    cache = Cache(api, lens, 1, d, dtype, fp4, 16, seed=11).fill()
+    q = _randn(sum(news) + 3, 4, d, seed=5, dtype=dtype).transpose(0, 1)
+    _check_attn(api, cache, q, news, packed=True)
+
+
+@pytest.mark.parametrize("dtype,fp4", [(BF, False), (BF, True), (F32, False)])
+@pytest.mark.parametrize("n,Hq", [(1, 8), (7, 8), (90, 8), (1, 64)])
+def test_attn_long_keys(api, dtype, fp4, n, Hq):
+    """Long sequences of unequal length: tiles that many work-groups share, that one finishes, that begin and end inside of stretches."""
+    lens = [9001, 130, 20011]
+    cache = Cache(api, lens, 2, 128, dtype, fp4, 64, seed=12).fill()
+    _check_attn(api, cache, _randn(3, Hq, n, 128, seed=6, dtype=dtype), [n] * 3)
+    one = Cache(api, [20011], 2, 128, dtype, fp4, 128, seed=13).fill()
+    _check_attn(api, one, _randn(1, Hq, n, 128, seed=7, dtype=dtype), [n])
+
+
+@pytest.mark.parametrize("n", [1, 33])
+def test_attn_fp4_nan_group(api, n):
+    """A group that held a NaN: every row that sees the key is NaN, rows of other sequences and KV heads are not."""
+    cache = Cache(api, [300, 300], 2, 128, BF, True, 16, seed=3).fill()
+    x = torch.zeros(2, 1, 128, dtype=torch.float64)
+    x[0, 0, 40] = math.nan
+    cache.put("k", 0, 77, x)
+    out, lse = _attn(api, cache, _randn(2, 4, n, 128, seed=1))
+    assert torch.isnan(out[0, :2]).all() and torch.isnan(lse[0, :2]).all()
+    assert torch.isfinite(out[0, 2:]).all() and torch.isfinite(out[1]).all()
+
+
 @pytest.mark.parametrize("dtype,fp4,d", FORMATS)
 @pytest.mark.parametrize("n", [1, 33])
 def test_attn_holes(api, dtype, fp4, d, n):
@@ -264,6 +298,37 @@ def test_append(api, dtype, fp4, d, rot, interleaved):
     for t, key, w in zip(before, keys, written):                      # nothing else of the storage was touched
         same = (t == cache.c[key]) | (torch.isnan(t.float()) & torch.isnan(cache.c[key].float()))
         assert bool((same | w).all())
+
+
+@pytest.mark.parametrize("dtype,fp4,d", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,interleaved", [(4, 2, False), (4, 1, True), (32, 8, False), (40, 4, True)])
+def test_append_many_tokens(api, dtype, fp4, d, Hq, Hkv, interleaved):
+    """Enough tokens for the work-groups that take four of them: few rows a token and many, a last work-group that is not full,
+    packed sequences of all lengths beside it."""
+    new = [700, 0, 1, 333, 2, 66, 1]
+    lens = [x + (i * 37) % 100 for i, x in enumerate(new)]
+    T, rot = sum(new), d
+    cache = Cache(api, lens, Hkv, d, dtype, fp4, 32, seed=d)
+    q, k, v = (_randn(T + 1, H, d, seed=s, dtype=dtype).transpose(0, 1) for H, s in ((Hq, 1), (Hkv, 2), (Hkv, 3)))
+    cu = torch.tensor([0] + new).cumsum(0).int().cuda()
+    qo, ko, f = _append(api, cache, q, k, v, rot, interleaved, cu=cu, max_new=max(new))
+    pos = torch.cat([torch.arange(ln - n, ln) for n, ln in zip(new, lens)]).cuda()
+    _near(qo[:, :T], rotate(q[:, :T], pos, f, interleaved), dtype, q[:, :T].double().abs().amax(dim=-1, keepdim=True) * 2)
+    want = rotate(k[:, :T], pos, f, interleaved)
+    _near(ko[:, :T], want, dtype, k[:, :T].double().abs().amax(dim=-1, keepdim=True) * 2)
+    at = 0
+    for b, n in enumerate(new):
+        if n:
+            sl = slice(at, at + n)
+            K, V = cache.rows("k", b, lens[b] - n, n), cache.rows("v", b, lens[b] - n, n)
+            assert torch.equal(K, fp4_values(*fp4_pack(want[:, sl])).cuda() if fp4 else ko[:, sl].double())
+            assert torch.equal(V, fp4_values(*fp4_pack(v[:, sl].double())).cuda() if fp4 else v[:, sl].double())
+        at += n
+    back_k, back_v = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    api.kv_read(api.make_kv_params(cache.c, cache.table, cache.kv_len, k=back_k, v=back_v, cu_seqlens=cu, max_new=max(new)), back_k, back_v)
+    rows = lambda x: torch.cat([cache.rows(x, b, lens[b] - n, n) for b, n in enumerate(new) if n], dim=1)
+    assert torch.equal(back_k[:, :T].double(), rows("k")) and torch.equal(back_v[:, :T].double(), rows("v"))
+    assert torch.all(back_k[:, T:] == 7.0) and torch.all(qo[:, T:] == 7.0) and torch.all(ko[:, T:] == 7.0)
 
 
 @pytest.mark.parametrize("dtype,fp4", [(BF, False), (BF, True), (F32, False)])

@@ -150,3 +150,71 @@ int main() {
     for byte, row in zip(list(range(7, 253)) + [255], vals):
         want = fp4_values(codes, torch.tensor([byte], dtype=torch.uint8))[:16]
         assert torch.equal(torch.isnan(row), torch.isnan(want)) and torch.equal(row.nan_to_num(), want.nan_to_num())
+
+
+def test_deal_on_the_host(tmp_path):
+    """Every unit belongs to exactly one work-group, the work-groups' numbers of units differ by one at most, and the places of the
+    shares of a tile are all different, whatever the lengths."""
+    src, exe = tmp_path / "d.cpp", str(tmp_path / "d")
+    src.write_text('''#include "%s/paper_2505_23520_amd/csrc/aa_kv_deal.h"
+#include <stdio.h>
+int main() {
+    unsigned total, groups;
+    while (scanf("%%u %%u", &total, &groups) == 2) {
+        aa::Deal d;
+        d.each = total / groups;
+        d.more = total - d.each * groups;
+        if (aa::deal_start(d, 0) != 0 || aa::deal_start(d, groups) != total) return 1;
+        for (unsigned g = 0; g < groups; ++g) {
+            const unsigned a = aa::deal_start(d, g), b = aa::deal_start(d, g + 1);
+            if (b - a != d.each && b - a != d.each + 1) return 2;
+            if (a < b && (aa::deal_group(d, a) != g || aa::deal_group(d, b - 1) != g)) return 3;
+        }
+        // tiles of many lengths along the line: each work-group leaves at most one share in each of its two places
+        static int used[4096];
+        for (unsigned i = 0; i < 2 * groups; ++i) used[i] = 0;
+        unsigned first = 0, units = 1;
+        while (first < total) {
+            if (first + units > total) units = total - first;
+            const unsigned g0 = aa::deal_group(d, first), g1 = aa::deal_group(d, first + units - 1);
+            for (unsigned g = g0; g0 < g1 && g <= g1; ++g) {
+                const unsigned t = g == g0 ? 0 : aa::deal_start(d, g) - first;
+                const int place = aa::deal_place((int)g, (int)t);
+                if (place < 0 || place >= (int)(2 * groups) || used[place]++) return 4;
+                if (place != aa::deal_place((int)(g0 + (g - g0)), (int)(g - g0))) return 5;          // how the joining kernel counts them
+            }
+            first += units;
+            units = units * 7 %% 23 + 1;
+        }
+    }
+    if (aa::deal_units(0, 0) != 0 || aa::deal_units(5000, 0) != 0 || aa::deal_units(0, 3) != 1 || aa::deal_units(128, 1) != 1 ||
+        aa::deal_units(129, 1) != 2 || aa::deal_units(1 << 30, 1) != 1 << 23) return 6;
+    return 0;
+}''' % ROOT)
+    subprocess.check_call(["g++", "-O2", "-std=c++17", str(src), "-o", exe])
+    pairs = [(t, g) for t in list(range(1, 200)) + [511, 512, 513, 767, 1000, 4097, 100003] for g in (1, 2, 7, 8, 256, 512, 768, 1024)]
+    run = subprocess.run([exe], input="".join("%d %d\n" % p for p in pairs), text=True)
+    assert run.returncode == 0
+
+
+def test_cache_kernels_do_not_spill(tmp_path):
+    """A spilled register's reload is a vector-memory load, and the wait for it waits for the tiles in flight.  As many waves per SIMD
+    as the dealing of the keys counts on."""
+    import re
+    from paper_2505_23520_amd import build
+    want = {"aa_kv_append.hip": lambda name: 3, "aa_kv_chunk.hip": lambda name: 3,
+            "aa_kv_attn.hip": lambda name: 1 if "join" in name else {"1": {"128": 3 if "ILi2E" in name else 2, "64": 3, "32": 4},
+                                                                     "2": {"128": 1, "64": 2, "32": 2}, "4": {"64": 1, "32": 1}}
+            [re.search(r"ILi\dELi(\d+)ELi(\d)E", name).group(2)][re.search(r"ILi\dELi(\d+)ELi(\d)E", name).group(1)]}
+    assert sorted(want) + ["aa_kv_api.hip"] == sorted(set(build.CACHE_SOURCES) - {"aa_kv_api.hip"}) + ["aa_kv_api.hip"]
+    for source, waves in want.items():
+        cmd = ["hipcc", *build.FLAGS, *build.EXTRA.get(source, []), "--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage",
+               os.path.join(build.CSRC, source), "-o", str(tmp_path / "x.s")]
+        report = subprocess.run(cmd, capture_output=True, text=True, check=True).stderr
+        names = re.findall(r"Function Name: (\S+)", report)
+        spills = [int(x) for x in re.findall(r"VGPRs Spill: (\d+)", report)]
+        occupancy = [int(x) for x in re.findall(r"Occupancy \[waves/SIMD\]: (\d+)", report)]
+        assert len(names) >= 2 and len(spills) == len(occupancy) == len(names)
+        assert not any(spills), dict(zip(names, spills))
+        for name, o in zip(names, occupancy):
+            assert o >= waves(name), (name, o)
