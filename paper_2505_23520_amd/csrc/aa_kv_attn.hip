@@ -311,7 +311,7 @@ template <int R> __device__ __forceinline__ Part part_of(const AttnArgs& p, int 
     x.b = b;
     x.sq = kv_seq(p.a, b);
     x.len = p.a.kv_len[b];
-    x.units = deal_units(seen(p.a, x.len, x.sq.n, x.sq.n - 1), x.sq.n);
+    x.units = p.whole ? x.sq.n > 0 : deal_units(seen(p.a, x.len, x.sq.n, x.sq.n - 1), x.sq.n);
     x.tiles = (x.sq.n * p.a.grp + R - 1) / R;
     return x;
 }
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
         const int stop = s.units - t < (int)(end - at) ? s.units : t + (int)(end - at);
         const int r0 = tile_no * R, rows = s.sq.n * a.grp, last = r0 + R < rows ? r0 + R - 1 : rows - 1;
         const int see_first = seen(a, s.len, s.sq.n, (int)p.by_grp.div(r0)), see_last = seen(a, s.len, s.sq.n, (int)p.by_grp.div(last));
-        const int hi = stop * kUnitKeys < see_last ? stop * kUnitKeys : see_last;
+        const int hi = !p.whole && stop * kUnitKeys < see_last ? stop * kUnitKeys : see_last;
         w.table = (const_int*)(a.table + s.b * a.table_stride);
         w.k = a.kc + hk * a.kcs[1] * unit; w.v = a.vc + hk * a.vcs[1] * unit;
         if constexpr (F == kRows4) { w.ks = a.ksc + hk * a.kss[1]; w.vs = a.vsc + hk * a.vss[1]; }
@@ -694,15 +694,21 @@ constexpr int kCUs = 256;
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room) {
     const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype), tiles = (rows + R - 1) / R;
     const long long items = tiles * B * Hkv;
-    KvSplit s = {0, 1, 0, 0};
+    KvSplit s = {0, 1, 0, 0, 0};
     if (R < kChunkRows) {
         // as many work-groups as run at once, or as there are units
         const int o = dtype == 0 ? (d == 32 ? occupancy<kRows32, 32>(R) : d == 64 ? occupancy<kRows32, 64>(R) : occupancy<kRows32, 128>(R))
                     : format ? (d == 64 ? occupancy<kRows4, 64>(R) : occupancy<kRows4, 128>(R))
                              : d == 64 ? occupancy<kRows16, 64>(R) : occupancy<kRows16, 128>(R);
-        const long long units = items * deal_units((int)longest, 1);
+        // Short sequences whole, without shares and the kernel that joins them (3 us, and its launch): a unit more costs a work-group
+        // 0.7 us, and takes longer than the join from five units on, unless there are enough tiles to fill the chip.  32 / 8 heads,
+        // bf16, shared / whole, us: 1 x 512 keys 9.4 / 9.1, 1 x 1000 9.6 / 13.4, 8 x 1000 15.9 / 14.6, 16 x 2000 28.2 / 24.7,
+        // 32 x 100 .. 1991 31.7 / 29.6, 64 x 512 26.3 / 24.1.
+        const int tile_units = deal_units((int)longest, 1);
+        s.whole = tile_units <= 4 || (tile_units <= 16 && items >= 8 * tile_units);
+        const long long units = items * (s.whole ? 1 : tile_units);
         s.groups = (int)(units < kCUs * o ? units : kCUs * o);
-        if (room > kUnitKeys) s.ws_bytes = 2ull * s.groups * R * (d + 2) * 4 + s.groups * sizeof(Shared);
+        if (!s.whole && room > kUnitKeys) s.ws_bytes = 2ull * s.groups * R * (d + 2) * 4 + s.groups * sizeof(Shared);
         return s;
     }
     // Row tiles through LDS: all tiles of a KV head begin their keys together, which is what lets an XCD's L2 serve them (dealt evenly like
@@ -725,7 +731,7 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     p.a = a;
     p.q = q; p.out = out; p.lse = lse;
     p.ws = sp.ws_bytes ? ws : nullptr;
-    p.groups = sp.groups; p.splits = sp.splits; p.chunk = sp.chunk;
+    p.groups = sp.groups; p.whole = sp.whole; p.splits = sp.splits; p.chunk = sp.chunk;
     p.rows = a.N * a.grp;
     const int R = tile_rows(p.rows, d, dtype);
     p.tiles = (p.rows + R - 1) / R;
