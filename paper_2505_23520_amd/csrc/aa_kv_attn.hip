@@ -713,10 +713,17 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
     }
     // Row tiles through LDS: all tiles of a KV head begin their keys together, which is what lets an XCD's L2 serve them (dealt evenly like
     // the others, 2048 and 1000 new tokens over 30011 and 8192 took 1148 us instead of 996).  Keys are split until there are as
-    // many work-groups as run at once, three a CU, or shares of 256 keys.  32 heads, 1024 and 403 new tokens over 16384 and 5003 in 4
-    // bits, work-groups wanted 512 / 768 / 2048: 529 / 369 / 489 us; 100 over 4000 in bf16: 26.2 / 26.0 / 37.
+    // many work-groups as run at once, three a CU, or shares of 256 keys, and up to twice as often where the fullest CU then has
+    // less to do: a CU takes 16.5 us for 1000 keys of a tile however many work-groups bring them, a share of 128 rows 0.027 us of the
+    // chip's memory time.  32 / 8 heads, 2 / 3 / 4 / 6 shares: 2 x 800 over 20000 keys 678 / 534 / 578 / 557 us; 1024 and 403 over 16384 and
+    // 5003 in 4 bits 369 / 382 / 433 / 382 (1: 529).
     long long splits = (kCUs * 3 + items - 1) / items;
     if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
+    auto cost = [&](long long n) {
+        return 16.5e-3 * (double)((items * n + kCUs - 1) / kCUs) * (double)((longest + n - 1) / n) + (n > 1 ? 4 + 0.027 * (double)(items * n) : 0.);
+    };
+    for (long long n = splits, most = 2 * splits + 2; n <= most && n * 512 <= longest; ++n)
+        if (cost(n) < cost(splits)) splits = n;
     if (splits > kMaxShares) splits = kMaxShares;
     const long long chunk = ((longest + splits - 1) / splits + 127) / 128 * 128;
     s.splits = (int)((longest + chunk - 1) / chunk);
