@@ -129,9 +129,10 @@ __device__ __forceinline__ long long uniform(long long x) {
            (long long)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
 }
 
-// TOKENS: of a work-group; TF of them, PASSES rows of each, are on their way in a thread at once.
-template <class T, bool FP4, int D, int PAIRS, int TOKENS, int TF, int PASSES>
-__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
+// TOKENS: of a work-group; PASSES rows of a token are on their way in a thread at once.
+// (4 bits, three passes: four waves a SIMD with a few registers in scratch memory, 16000 tokens of 48 rows 115 us; three without, 118.)
+template <class T, bool FP4, int D, int PAIRS, int TOKENS, int PASSES>
+__global__ __launch_bounds__(256, (FP4 && PASSES == 3 ? 4 : 1)) void kv_append_kernel(AppendArgs p) {
     constexpr int V = kVec<T>, LANES = D / V, ROWS = 256 / LANES, item = sizeof(T);
     using S = typename std::conditional<FP4, double, float>::type;
     __shared__ S s_cs[TOKENS][D / 2][2];
@@ -165,44 +166,35 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
     const int f0 = !turn ? 0 : PAIRS == kNeighbours ? c / 2 : upper ? c - half : c;
     for (int r0 = threadIdx.x / LANES + ROWS * PASSES * blockIdx.y; r0 < rows + threadIdx.x / LANES; r0 += ROWS * PASSES * gridDim.y) {
         // where a thread's rows lie from the token's on
-        bool is_q[PASSES], is_v[PASSES], there[PASSES];
+        bool is_q[PASSES], is_v[PASSES];
         long long from[PASSES], to[PASSES], pool[PASSES];
-        int head[PASSES];
 #pragma unroll
         for (int u = 0; u < PASSES; ++u) {
             const int r = r0 + u * ROWS < rows ? r0 + u * ROWS : rows - 1;
-            there[u] = r0 + u * ROWS < rows;
             is_q[u] = r < nq;
             is_v[u] = r >= nq + nk;
             const int h = is_q[u] ? r : is_v[u] ? r - nq - nk : r - nq;
-            head[u] = h;
             from[u] = (long long)h * (is_q[u] ? a.qs[1] : is_v[u] ? a.vs[1] : a.ks[1]) + c;
             to[u] = (long long)h * (is_q[u] ? a.os[1] : a.kos[1]) + c;
             pool[u] = (long long)h * (is_v[u] ? a.vcs[1] : a.kcs[1]) + (FP4 ? c / 2 : c);
         }
 #pragma unroll 1
-        for (int tk0 = 0; tk0 < TOKENS; tk0 += TF) {
-            u32x4 x[TF][PASSES], z[TF][PASSES];
+        for (int tk = 0; tk < TOKENS; ++tk) {
+            const int i = __builtin_amdgcn_readfirstlane(s_tok[tk].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk].b);
+            if (i < 0) continue;
+            const long long row0 = uniform(s_tok[tk].row0);
+            const T* q = (const T*)p.q + kv_row(a, a.qs, b, row0, i, 0);
+            const T* k = (const T*)p.k + kv_row(a, a.ks, b, row0, i, 0);
+            const T* v = (const T*)p.v + kv_row(a, a.vs, b, row0, i, 0);
+            u32x4 x[PASSES], z[PASSES];
 #pragma unroll
-            for (int f = 0; f < TF; ++f) {
-                const int i = __builtin_amdgcn_readfirstlane(s_tok[tk0 + f].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk0 + f].b);
-                if (i < 0) continue;
-                const long long row0 = uniform(s_tok[tk0 + f].row0);
-                const T* q = (const T*)p.q + kv_row(a, a.qs, b, row0, i, 0);
-                const T* k = (const T*)p.k + kv_row(a, a.ks, b, row0, i, 0);
-                const T* v = (const T*)p.v + kv_row(a, a.vs, b, row0, i, 0);
-#pragma unroll
-                for (int u = 0; u < PASSES; ++u) {
-                    const T* src = (is_q[u] ? q : is_v[u] ? v : k) + from[u];
-                    x[f][u] = *(const u32x4*)src;
-                    if (PAIRS == kHalves) z[f][u] = *(const u32x4*)(src + other);
-                }
+            for (int u = 0; u < PASSES; ++u) {
+                const T* src = (is_q[u] ? q : is_v[u] ? v : k) + from[u];
+                x[u] = *(const u32x4*)src;
+                if (PAIRS == kHalves) z[u] = *(const u32x4*)(src + other);
             }
-#pragma unroll
-            for (int f = 0; f < TF; ++f) {
-                const int tk = tk0 + f;
+            {                                                // (the token once more: kept, it takes registers of the rows in flight)
                 const int i = __builtin_amdgcn_readfirstlane(s_tok[tk].i), b = __builtin_amdgcn_readfirstlane(s_tok[tk].b);
-                if (i < 0) continue;
                 const int page = __builtin_amdgcn_readfirstlane(s_tok[tk].page), in = __builtin_amdgcn_readfirstlane(s_tok[tk].in);
                 const long long row0 = uniform(s_tok[tk].row0);
                 float cs[V], sn[V];
@@ -222,15 +214,15 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
 #pragma unroll
                 for (int u = 0; u < PASSES; ++u) {
                     float y[V], m[V];
-                    unpack<T>(x[f][u], y);
+                    unpack<T>(x[u], y);
                     if (PAIRS == kHalves) {
-                        unpack<T>(z[f][u], m);
+                        unpack<T>(z[u], m);
                     } else {
 #pragma unroll
                         for (int e = 0; e < V; ++e) m[e] = y[e ^ 1];
                     }
                     const bool turned = turn && !is_v[u];
-                    u32x4 w = x[f][u];
+                    u32x4 w = x[u];
                     float t[V];
                     if (PAIRS != kNoPairs) {
 #pragma unroll
@@ -239,7 +231,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) w[e] = turned ? r[e] : w[e];
                     }
-                    if (!there[u]) continue;
+                    if (r0 + u * ROWS >= rows) continue;
                     if (is_q[u]) {
                         *(u32x4*)(qo + to[u]) = w;
                         continue;
@@ -261,8 +253,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs p) {
                         int byte;
                         *(unsigned*)((is_v[u] ? vc : kc) + pool[u]) = to_fp4(y, &byte);
                         if (c % kFp4Group) continue;
-                        unsigned char* sc = is_v[u] ? a.vsc + page * a.vss[0] + head[u] * a.vss[1] + c / kFp4Group * a.vss[2]
-                                                    : a.ksc + page * a.kss[0] + head[u] * a.kss[1] + c / kFp4Group * a.kss[2];
+                        const int h = r0 + u * ROWS - nq - (is_v[u] ? nk : 0);
+                        unsigned char* sc = is_v[u] ? a.vsc + page * a.vss[0] + h * a.vss[1] + c / kFp4Group * a.vss[2]
+                                                    : a.ksc + page * a.kss[0] + h * a.kss[1] + c / kFp4Group * a.kss[2];
                         sc[in] = (unsigned char)byte;
                     }
                 }
@@ -332,12 +325,18 @@ template <class T, bool FP4, int D, int PAIRS>
 int run_pairs(const AppendArgs& p, hipStream_t st) {
     constexpr int ROWS = 256 / (D / kVec<T>);                      // rows of a token that a work-group takes at once
     const int rows = (p.q_out ? p.a.Hq : 0) + (p.k ? 2 * p.a.Hkv : 0);
-    const dim3 block(256), few((unsigned)p.a.total, (rows + 3 * ROWS - 1) / (3 * ROWS)), many((unsigned)((p.a.total + 3) / 4));
-    // Few tokens: a work-group for three passes over a token's rows, so that none waits for another.
-    if (p.a.total < 1024) return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1, 1, 3>, dim3(few.x, few.y < 64 ? few.y : 64), block, 0, st, p);
-    // Few rows: those of four tokens on their way instead of three passes of one.
-    if (rows <= ROWS) return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 4, 1>, many, block, 0, st, p);
-    return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 1, 3>, many, block, 0, st, p);
+    // A work-group a token, or four of them: what is worked out once a work-group is shared by more, but a token waits for the one before.
+    // A token / four, us, d = 128, tokens 300, 2000, 8000, 51000; plain pages, 48 rows (32 / 8 heads) 5.2 / 8.4, 12.3 / 13.4, 44.3 / 48.2,
+    // 253 / 266; 24 rows (8 / 8) 4.6 / 7.2, 9.7 / 10.6, 23.5 / 22.5, 164 / 146; 8 rows (4 / 2) 4.3 / 5.9, 7.7 / 7.5, 21.5 / 16.4, 126 / 81;
+    // 4 bits, where the angles take 64 bits to the end, 48 rows 11.1 / 15.4, 23.4 / 21.9, 66 / 64, 371 / 351; 8 rows 9.8 / 12.1, 15.4 / 13.5,
+    // 42 / 26, 231 / 128.
+    if (p.a.total < (FP4 || rows <= ROWS ? 2000 : 4000) || (!FP4 && rows > 2 * ROWS)) {
+        const int passes = (rows + 3 * ROWS - 1) / (3 * ROWS);
+        return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1, 3>, dim3((unsigned)p.a.total, passes < 64 ? passes : 64), dim3(256), 0, st, p);
+    }
+    const dim3 grid((unsigned)((p.a.total + 3) / 4));
+    if (rows <= ROWS) return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 1>, grid, dim3(256), 0, st, p);
+    return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 4, 3>, grid, dim3(256), 0, st, p);
 }
 template <class T, bool FP4, int D>
 int run_append(const AppendArgs& p, hipStream_t st) {

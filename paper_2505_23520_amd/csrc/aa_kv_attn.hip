@@ -55,7 +55,7 @@ template <int D> struct Tile<kRows32, D> {
 };
 
 // Waves of a SIMD that a kernel's registers allow, and so work-groups of a CU.
-template <int F, int D, int NT> constexpr int kOccupancy = NT == 1 ? (D == 128 ? (F == kRows4 ? 3 : 2) : D == 64 ? 3 : 4) : NT == 2 && D < 128 ? 2 : 1;
+template <int F, int D, int NT> constexpr int kOccupancy = NT == 1 ? (D == 128 ? (F == kRows4 ? 3 : 2) : D == 64 ? 3 : 4) : NT == 2 && (D < 128 || F == kRows4) ? 2 : 1;
 
 // What a wave needs to find a tile: its sequence's pages, the pools from its head on, and a lane's place in 16 keys (bytes).
 struct Where {
@@ -654,11 +654,17 @@ __global__ __launch_bounds__(256) void kv_join_one_kernel(AttnArgs p) {
                       (T*)p.out + kv_row(a, a.os, 0, s.sq.row0, i, h), p.lse ? p.lse + lse_of(a, s.sq, 0, h, i) : nullptr);
 }
 
-// Rows of a work-group: 16 or 32 a wave's registers hold beside two tiles of d = 128; more go through LDS, 128 at a time, or 64 where d is
-// less (float: 32, there is no such kernel).
-int tile_rows(long long rows, int d, int dtype) {
+// Rows of a work-group.  More rows share a key that is read once, but take registers from the tiles in flight; 128 share it through LDS.
+// 32 / 8 heads, d = 128, rows of a KV head and us with 16 / 32 / 128 rows a work-group:
+//   32 sequences, 0.24 M keys, bf16   4: 141 / 144 / 169   16: 148 / 149 / 173   20: 232 / 153 / 177   36: 334 / 252 / 186
+//   2 sequences, 25000 keys, bf16     4: 25.8 / 27.5 / 24.9   20: 40.5 / 30.3 / 25.8   64: 67.6 / 43.8 / 30.9
+//   64 sequences, 0.53 M keys, 4 bits   8: 125 / 147 / 478   32: 202 / 151 / 485   36: 279 / 252 / 503   64: 371 / 256 / 511
+//   1 sequence, 30000 keys, 4 bits    120: 51.4 / 42.6 / 43.1
+// (LDS: the conversion of 4 bits and the matrix products of 128 rows take their time however few rows there are.)  d = 64, 4 x 8000 keys:
+// 2000 rows, 16 / 32 / 64 rows 195 / 153 / 92.  Float has no kernel through LDS.
+int tile_rows(long long rows, int d, int dtype, int format) {
     if (rows <= 16) return 16;
-    if (rows <= 32 || (d == 128 && dtype == 0)) return 32;
+    if (rows <= 32 || (d == 128 && dtype == 0) || (d == 128 && format && rows <= 64)) return 32;
     return d == 128 ? kChunkRows : 64;
 }
 
@@ -692,7 +698,7 @@ constexpr int kCUs = 256;
 }  // namespace
 
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room) {
-    const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype), tiles = (rows + R - 1) / R;
+    const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype, format), tiles = (rows + R - 1) / R;
     const long long items = tiles * B * Hkv;
     KvSplit s = {0, 1, 0, 0, 0};
     if (R < kChunkRows) {
@@ -740,7 +746,7 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     p.ws = sp.ws_bytes ? ws : nullptr;
     p.groups = sp.groups; p.whole = sp.whole; p.splits = sp.splits; p.chunk = sp.chunk;
     p.rows = a.N * a.grp;
-    const int R = tile_rows(p.rows, d, dtype);
+    const int R = tile_rows(p.rows, d, dtype, format);
     p.tiles = (p.rows + R - 1) / R;
     p.c = a.sigma * kLog2e;
     p.slack = fminf(8.f / p.c, 3.402823466e38f);
