@@ -52,10 +52,30 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     // ---- loader role: keys 16 wave .. 16 wave + 15 of a tile
     const_int* table = (const_int*)(a.table + w.b * a.table_stride);
     const long long room = (long long)a.max_pages << a.page_shift;
-    auto page_at = [&](int j) -> int {               // of key j; -1: none
-        if (j >= room) return -1;
-        const int x = table[j >> a.page_shift];
-        return (unsigned)x < (unsigned)a.n_pages ? x : -1;
+    // Pages of a tile: the wave's own, and which of the four groups of 16 keys have one.  The entries are requested two tiles ahead, in the
+    // softmax, where nothing else is in flight in the scalar and LDS units: a scalar load on its way while operands are read from
+    // LDS would turn every wait for one of them into a wait for all (looked up at the tile's start: 1032 us for 1014 us here).
+    struct Entries { int x[4]; };
+    struct Pages { int own; unsigned there; };
+    auto entries_of = [&](int t) -> Entries {
+        Entries e;
+        const int j = w.lo + TK * t;
+        e.x[0] = j < room ? table[j >> a.page_shift] : -1;
+        e.x[1] = e.x[2] = e.x[3] = e.x[0];
+        if (__builtin_expect(a.page_shift < 6, 0)) {
+#pragma unroll
+            for (int i = 1; i < 4; ++i) e.x[i] = j + 16 * i < room ? table[(j + 16 * i) >> a.page_shift] : -1;
+        }
+        return e;
+    };
+    auto pages_of = [&](const Entries& e) -> Pages {
+        Pages g;
+        g.there = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g.there |= (unsigned)((unsigned)e.x[i] < (unsigned)a.n_pages) << i;
+        const int x = wave == 0 ? e.x[0] : wave == 1 ? e.x[1] : wave == 2 ? e.x[2] : e.x[3];
+        g.own = g.there >> wave & 1 ? x : -1;
+        return g;
     };
     auto key_of = [&](int t) -> int { return w.lo + TK * t + 16 * wave; };
     const char* const k0 = a.kc + w.hk * a.kcs[1] * (FP4 ? 1 : 2);
@@ -124,7 +144,8 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     const int ls = lane & 15, lg = lane >> 4;
     const int voff = (4 * hf + (ls >> 2)) * VGRP + 32 * (lg & 1) + 8 * (ls & 3);
 
-    int pg = page_at(key_of(0)), pg_next = nT > 1 ? page_at(key_of(1)) : -1;
+    Pages now = pages_of(entries_of(0)), next = pages_of(entries_of(1));
+    const int pg = now.own;
     Codes kc, vc;
     if (nT > 0) {
         if constexpr (FP4) {
@@ -142,19 +163,16 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
     auto tile_step = [&](int t, const char* Kcur, char* Knext) __attribute__((always_inline)) {
         const int t0 = w.lo + TK * t, j = key_of(t);
         if constexpr (FP4) codes_store(vc, Vs0, VGRP);
-        else rows_load(base_of(v0, a.vcs, j, pg), vstb, Vs0, VGRP);
+        else rows_load(base_of(v0, a.vcs, j, now.own), vstb, Vs0, VGRP);
         __builtin_amdgcn_sched_barrier(0);
-        // the pages of the whole tile, for the masks
-        unsigned there = 0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) there |= (page_at(t0 + 16 * x) >= 0) << x;
+        const unsigned there = now.there;
         const bool whole = there == 15 && t0 + TK <= w.hi;
         const bool on = t0 < see_wave_last && rw < w.rows;
         const char* Kb = Kcur + koff;
         const char* Vb = Vs0 + voff;
         bf16x8 pf[2][2];
+        floatx16 s[2];
         if (on) {
-            floatx16 s[2];
             {
                 bf16x8 kf[16];
                 auto read_k = [&](int i) { kf[i] = *(const bf16x8*)(Kb + 512 * (i & 1) + 32 * (i >> 1)); };
@@ -179,13 +197,18 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
                         s[kb][v] = ok ? s[kb][v] : -INFINITY;
                     }
             }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const Entries ahead = entries_of(t + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (on) {
             __builtin_amdgcn_s_setprio(0);
             softmax_tile(s, pf, c2, gap, mref, mtrue, l, o);
             __builtin_amdgcn_s_setprio(2);
         }
         __builtin_amdgcn_sched_barrier(0);
         // the next K tile (past the end the last one again, into a stage that nobody reads)
-        const int u = t + 1 < nT ? t + 1 : t, ju = key_of(u), pu = t + 1 < nT ? pg_next : pg;
+        const int u = t + 1 < nT ? t + 1 : t, ju = key_of(u), pu = t + 1 < nT ? next.own : now.own;
         if constexpr (FP4) {
             kc = codes_load(base_of(k0, a.kcs, ju, pu), kstb, a.ksc, a.kss, ju, pu);
             vc = codes_load(base_of(v0, a.vcs, ju, pu), vstb, a.vsc, a.vss, ju, pu);
@@ -233,8 +256,8 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
             wait_vmem();                             // the next K tile has landed
         }
         chunk_barrier();
-        pg = pu;
-        pg_next = t + 2 < nT ? page_at(key_of(t + 2)) : -1;
+        now = next;
+        next = pages_of(ahead);
     };
     for (int t = 0; t < nT; t += 2) {
         tile_step(t, Ks0, Ks1);
