@@ -13,9 +13,6 @@ bool unaligned(const void* ptr) { return ((uintptr_t)ptr & 15) != 0; }
 // Strides of a tensor of new tokens: multiples of 16 bytes; `out`: no two rows of it in one place.
 int check_rows(const aa_kv_params* p, const int64_t* st, int heads, bool out) {
     const int vec = p->dtype == AA_BF16 ? 8 : 4;
-    // units of all rows (see aa_kv_deal.h) are counted in 32 bits
-    if ((int64_t)p->B * p->Hkv > (1ll << 31) / ((int64_t)p->max_pages * p->page_size / 128 + 1) / (((int64_t)p->N * (p->Hq / p->Hkv) + 15) / 16 + 1))
-        return AA_EUNSUPPORTED;
     const int64_t tokens = p->cu_seqlens ? p->total_tokens : p->N;
     for (int e = 0; e < 3; ++e)
         if (!(e == 0 && p->cu_seqlens) && (st[e] < 0 || st[e] % vec || st[e] >= (1ll << 40))) return AA_EINVAL;
@@ -59,13 +56,13 @@ int make_args(const aa_kv_params* p, KvArgs* a) {
     if (p->page_size < 16 || p->page_size > (1 << 20)) return AA_EUNSUPPORTED;
     if (p->rot_dim % 16) return AA_EUNSUPPORTED;
     if ((int64_t)p->max_pages * p->page_size > (1 << 30)) return AA_EUNSUPPORTED;       // tokens of a sequence are counted in 32 bits
-    // heads and sequences stand on y and z of a launch grid, tokens on x; new rows of a KV head stay below 2^31
+    // sequences stand on y of a launch grid, a work-group of 256 threads for every token on x, whose threads are counted in 32 bits
     if (p->B > 65535 || p->Hq > 65535) return AA_EUNSUPPORTED;
     // units of all rows (see aa_kv_deal.h) are counted in 32 bits
     if ((int64_t)p->B * p->Hkv > (1ll << 31) / ((int64_t)p->max_pages * p->page_size / 128 + 1) / (((int64_t)p->N * (p->Hq / p->Hkv) + 15) / 16 + 1))
         return AA_EUNSUPPORTED;
     const int64_t tokens = p->cu_seqlens ? p->total_tokens : (int64_t)p->B * p->N;
-    if (tokens >= (1ll << 31) || (int64_t)p->N * (p->Hq / p->Hkv) >= (1ll << 30)) return AA_EUNSUPPORTED;
+    if (tokens >= (1 << 24) || (int64_t)p->N * (p->Hq / p->Hkv) >= (1ll << 30)) return AA_EUNSUPPORTED;
     int rc = check_pool(p, p->kc, p->kc_stride, p->ks, p->ks_stride);
     if (rc == AA_OK) rc = check_pool(p, p->vc, p->vc_stride, p->vs, p->vs_stride);
     if (rc != AA_OK) return rc;

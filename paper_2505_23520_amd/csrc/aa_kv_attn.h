@@ -12,6 +12,7 @@ struct AttnArgs {
     float *lse, *ws;
     int rows, tiles;                 // most rows of a KV head and sequence (N * grp), their row tiles
     int groups, whole;               // registers: work-groups that the line of units is dealt to; whole: a tile is one unit, however long
+    int tell;                        // registers: the work-groups tell the joining kernel which tiles are shared
     int splits, chunk;               // LDS: work-groups of a row tile, keys of each (the last one's: what is left)
     float c;                         // sigma * log2 e
     float slack;                     // a reference is raised when a score exceeds it by this much: weights stay below 2^8

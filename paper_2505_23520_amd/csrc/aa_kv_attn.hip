@@ -402,7 +402,7 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
     Line<R> line(p);
     if (a.B == 1) head_units = (unsigned)s.units * s.tiles;
     else head_units = line.units();
-    Shared* const told = p.ws && a.B > 1 ? shared_tiles(p, R, D) + blockIdx.x : nullptr;
+    Shared* const told = p.tell ? shared_tiles(p, R, D) + blockIdx.x : nullptr;
     if (told && threadIdx.x == 0) told->count = 0;
     const unsigned total = head_units * a.Hkv;
     const Deal deal = deal_of(p, total);
@@ -615,7 +615,7 @@ __global__ __launch_bounds__(256) void kv_join_rows_kernel(AttnArgs p) {
                       nullptr, (T*)p.out + kv_row(a, a.os, b, sq.row0, i, h), p.lse ? p.lse + lse_of(a, sq, b, h, i) : nullptr);
 }
 
-// kv_attn_kernel's shares of several sequences: its work-groups tell which tiles are shared; a work-group for four rows of each.
+// kv_attn_kernel's shares of many row tiles: its work-groups tell which tiles are shared; a work-group for four rows of each.
 template <class T, int D, int R>
 __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
     __shared__ float s_w[4][kMaxShares];
@@ -634,7 +634,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(AttnArgs p) {
                       p.lse ? p.lse + lse_of(a, sq, told.b, h, i) : nullptr);
 }
 
-// Of one sequence: where a tile's units are dealt to is known without being told, and a tile has many shares; a work-group a row.
+// Of one sequence with few row tiles: where a tile's units are dealt to is known without being told, and it has many shares; a
+// work-group a row.
 template <class T, int D, int R>
 __global__ __launch_bounds__(256) void kv_join_one_kernel(AttnArgs p) {
     __shared__ float s_w[4][kMaxShares];
@@ -668,27 +669,28 @@ int tile_rows(long long rows, int d, int dtype, int format) {
     return d == 128 ? kChunkRows : 64;
 }
 
+constexpr long long kMaxGrid = 1ll << 24;     // work-groups of 256 threads: a launch counts its threads in 32 bits
+
 template <int F, int D, int NT>
 int run_registers(const AttnArgs& p, hipStream_t st) {
     using T = typename RowType<F>::type;
     int e = (int)launch_kernel(kv_attn_kernel<F, D, NT>, dim3(p.groups), dim3(64 * kWaves), 0, st, p);
     if (e != (int)hipSuccess || !p.ws) return e;
-    if (p.a.B == 1) return (int)launch_kernel(kv_join_one_kernel<T, D, 16 * NT>, dim3((unsigned)p.a.Hkv * p.rows), dim3(256), 0, st, p);
+    if (!p.tell) return (int)launch_kernel(kv_join_one_kernel<T, D, 16 * NT>, dim3((unsigned)p.a.Hkv * p.rows), dim3(256), 0, st, p);
     return (int)launch_kernel(kv_join_kernel<T, D, 16 * NT>, dim3(p.groups, ((p.rows < 16 * NT ? p.rows : 16 * NT) + 3) / 4), dim3(256), 0, st, p);
 }
 
 template <int F, int D>
 int run(const AttnArgs& p, int R, hipStream_t st) {
     using T = typename RowType<F>::type;
-    if ((long long)p.a.Hkv * p.rows > 0x7fffffffll) return -1;
     if (R == 16) return run_registers<F, D, 1>(p, st);
     if (R == 32) return run_registers<F, D, 2>(p, st);
     if constexpr (D < 128) return run_registers<F, D, 4>(p, st);
-    const long long x = (long long)p.a.Hkv * p.tiles * p.splits;
-    if (x > 0x7fffffffll) return -1;
+    const long long x = (long long)p.a.Hkv * p.tiles * p.splits, join = p.splits == 1 ? 1 : (long long)p.a.Hkv * ((p.rows + 3) / 4);
+    if (x >= kMaxGrid || join >= kMaxGrid) return -1;
     const int e = launch_kv_chunk(p, F == kRows4, dim3((unsigned)x, p.a.B), st);
     if (e != (int)hipSuccess || p.splits == 1) return e;
-    return (int)launch_kernel(kv_join_rows_kernel<T, D>, dim3((unsigned)p.a.Hkv * ((p.rows + 3) / 4), p.a.B), dim3(256), 0, st, p);
+    return (int)launch_kernel(kv_join_rows_kernel<T, D>, dim3((unsigned)join, p.a.B), dim3(256), 0, st, p);
 }
 
 template <int F, int D> int occupancy(int R) { return R == 16 ? kOccupancy<F, D, 1> : R == 32 ? kOccupancy<F, D, 2> : kOccupancy<F, D, 4>; }
@@ -748,6 +750,9 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     p.rows = a.N * a.grp;
     const int R = tile_rows(p.rows, d, dtype, format);
     p.tiles = (p.rows + R - 1) / R;
+    // Being told costs one sequence with few tiles more than it saves; 16000 keys of 8 KV heads, d = 64, 13 / 63 tiles, untold / told
+    // 82 / 80, 308 / 292 us; 2 tiles of 30000 keys in 4 bits 29 / 32, 8 of 8000 in float 36.5 / 39.6.
+    p.tell = p.ws && (a.B > 1 || p.tiles > 8 || (long long)a.Hkv * p.rows >= kMaxGrid);
     p.c = a.sigma * kLog2e;
     p.slack = fminf(8.f / p.c, 3.402823466e38f);
     p.by_hkv.set(a.Hkv); p.by_splits.set(sp.splits); p.by_grp.set(a.grp); p.by_groups.set(sp.groups ? sp.groups : 1);

@@ -112,6 +112,25 @@ def test_attn_long_keys(api, dtype, fp4, n, Hq):
     _check_attn(api, one, _randn(1, Hq, n, 128, seed=7, dtype=dtype), [n])
 
 
+@pytest.mark.parametrize("dtype,fp4,d", [(BF, False, 64), (BF, True, 64), (F32, False, 128), (F32, False, 64), (BF, True, 128), (BF, False, 128)])
+@pytest.mark.parametrize("n,length", [(9, 4000), (24, 4000), (150, 3000), (700, 700)])
+def test_attn_one_sequence_many_rows(api, dtype, fp4, d, n, length):
+    """One sequence whose rows take several row tiles, the keys of each in shares."""
+    cache = Cache(api, [length], 2, d, dtype, fp4, 64, seed=n).fill()
+    _check_attn(api, cache, _randn(1, 8, n, d, seed=n, dtype=dtype), [n])
+
+
+@pytest.mark.parametrize("dtype,fp4", [(BF, False), (BF, True), (F32, False)])
+@pytest.mark.parametrize("n", [1, 40])
+def test_attn_shared_pages(api, dtype, fp4, n):
+    """Two sequences on the pages of one prefix, and a sequence that has a page twice."""
+    lens = [700, 650, 300]
+    cache = Cache(api, lens, 2, 128, dtype, fp4, 32, seed=2).fill()
+    cache.table[1, :15] = cache.table[0, :15]
+    cache.table[2, 5] = cache.table[2, 1]
+    _check_attn(api, cache, _randn(3, 8, n, 128, seed=n, dtype=dtype), [n] * 3)
+
+
 @pytest.mark.parametrize("n", [1, 33])
 def test_attn_fp4_nan_group(api, n):
     """A group that held a NaN: every row that sees the key is NaN, rows of other sequences and KV heads are not."""
@@ -514,11 +533,60 @@ def test_captured_step_replays(api, dtype, fp4):
 
 
 @pytest.mark.parametrize("dtype,fp4", [(BF, False), (BF, True), (F32, False)])
-def test_two_streams_and_repeats(api, dtype, fp4):
+def test_captured_chunk_replays(api, dtype, fp4):
+    """A packed chunk captured into a graph and replayed with other splits of the same rows, other lengths and other inputs."""
+    Hq, Hkv, d, total = 8, 2, 128, 400
+    cache = Cache(api, [3000, 500, 400], Hkv, d, dtype, fp4, 16, seed=4).fill()
+    q, k, v = (_randn(H, total, d, seed=s, dtype=dtype) for H, s in ((Hq, 1), (Hkv, 2), (Hkv, 3)))
+    f = torch.rand(d // 2, device="cuda")
+    cu = torch.tensor([0, 100, 150, 390], dtype=torch.int32, device="cuda")
+    qo, out, ko, vo = (torch.empty_like(x) for x in (q, q, k, v))
+    lse = torch.empty(Hq * total, device="cuda")
+    kw = dict(cu_seqlens=cu, max_new=300)
+    pa = api.make_kv_params(cache.c, cache.table, cache.kv_len, q=q, k=k, v=v, out=qo, rot_dim=d, **kw)
+    pt = api.make_kv_params(cache.c, cache.table, cache.kv_len, q=qo, out=out, **kw)
+    pr = api.make_kv_params(cache.c, cache.table, cache.kv_len, k=ko, v=vo, **kw)
+    ws = torch.empty(api.kv_attn_workspace_bytes(pt), dtype=torch.uint8, device="cuda")
+
+    def step():
+        api.kv_append(pa, q, k, v, f, None, qo)
+        api.kv_attn(pt, qo, out, lse, ws)
+        api.kv_read(pr, ko, vo)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for t, (ends, lens) in enumerate((([0, 100, 150, 390], [3000, 500, 400]), ([0, 0, 300, 400], [77, 301, 100]), ([0, 1, 2, 3], [2900, 0, 399]),
+                                      ([0, 300, 300, 320], [300, 400, 20]))):
+        cache.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        cu.copy_(torch.tensor(ends, dtype=torch.int32))
+        q.copy_(_randn(Hq, total, d, seed=20 + t, dtype=dtype))
+        k.copy_(_randn(Hkv, total, d, seed=40 + t, dtype=dtype))
+        results = [out, lse, ko, vo]
+        for x in results:
+            x.fill_(7.0)
+        step()
+        want = [x.clone() for x in results] + _storage(cache)
+        for x in results:
+            x.fill_(7.0)
+        ws.fill_(0xff)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.all(out[:, ends[-1]:] == 7.0)
+        for a, b in zip(want, results + _storage(cache)):
+            assert torch.equal(a.float().nan_to_num(), b.float().nan_to_num())
+
+
+@pytest.mark.parametrize("n", [1, 90])
+@pytest.mark.parametrize("dtype,fp4", [(BF, False), (BF, True), (F32, False)])
+def test_two_streams_and_repeats(api, dtype, fp4, n):
     """Two calls at once, each with its workspace, on streams other than the tensors' own: the bits of calls one after the other."""
     d = 128
     caches = [Cache(api, lens, 2, d, dtype, fp4, 32, seed=s).fill(seed=s) for s, lens in ((1, [3000, 5]), (2, [1200, 2500]))]
-    qs = [_randn(2, 8, 1, d, seed=s, dtype=dtype) for s in (1, 2)]
+    qs = [_randn(2, 8, n, d, seed=s, dtype=dtype) for s in (1, 2)]
     want = [_attn(api, c, q) for c, q in zip(caches, qs)]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
