@@ -1,7 +1,6 @@
 // The 4-bit format of cached rows: a sign, two exponent bits and one of mantissa, and a power-of-two scale for 32 channels.
 // The same code on the host, where it is compared with the definition.
 #pragma once
-#include <math.h>
 #include <stdint.h>
 
 #ifdef __HIPCC__
@@ -24,14 +23,6 @@ AA_HD int fp4_scale_byte(uint32_t top) {
     if (ex == 255) return 255;
     const int e = ex - 127 - 2 + ((top & 0x7fffffu) > 0x600000u);
     return 127 + (e < -120 ? -120 : e > 125 ? 125 : e);
-}
-
-// The value of a code under a scale byte.
-AA_HD float fp4_value(unsigned code, int byte) {
-    if (byte == 255) return NAN;
-    const int e = (code >> 1) & 3, m = code & 1;
-    const float a = e == 0 ? 0.5f * m : (float)((2 + m) << (e - 1)) * 0.5f;
-    return (code & 8 ? -a : a) * exp2f((float)byte - 127.0f);
 }
 
 }  // namespace aa
