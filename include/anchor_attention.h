@@ -304,6 +304,8 @@ int kv_attn_workspace_bytes(const aa_kv_params *params, size_t *bytes_out);
  * storage that no row of a sequence sees (behind its end, other pages) never reaches an output, whatever its bits; a value row that
  * is not finite reaches every row of its sequence that it is computed with.  out and q must not overlap, and a call has its workspace
  * for itself until it is through.
+ * Equal calls give equal bits.  The order of a row's sums depends on how the call's keys are dealt out, and so on the lengths of its
+ * other sequences and on max_len.
  */
 int kv_attn(const aa_kv_params *params, const void *q, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 

@@ -1,9 +1,14 @@
 // kv_append and kv_read: rows of new tokens into the pages of the cache (rotated on the way) and out of them.
 //
+//   y1 = x1 cos t - x2 sin t,  y2 = x2 cos t + x1 sin t,  t = position * inv_freq[pair]
+//
 // Memory traffic is all that they cannot do without: every row is read once and written once or twice, at some six operations an
-// element.  A work-group takes four tokens (one where there are few): each of its waves works out where a token lies and the cosines and
-// sines of its position, one angle a lane, for all heads; then the threads take 16 bytes of a row each, the rows of a token that one
-// thread meets being in flight together.
+// element.  A work-group takes a token, or four (see run_pairs): a wave for each works out where it lies and the cosines and sines of its
+// position, one angle a lane, for all heads; then the threads take 16 bytes of a row each, a pair's other half being read a
+// second time from the L1, and the rows of a token that one thread meets are in flight together.
+// 51393 tokens of 32 / 8 heads, d = 128, bf16: 1.37 GB in 263 us, 5.2 TB/s (a copy of 4 GB: 4.7).  16384 tokens into 4 bits: 0.39 GB in
+// 97 us, 4.0 TB/s, the 64-bit turning of the keys standing beside the traffic; kv_read of them 85 MB in 21 us, 4.0 TB/s.  One token: 3.4 us,
+// which is a launch and four dependent reads (length, page, then the row).
 #include <type_traits>
 
 #include "aa_kv.h"

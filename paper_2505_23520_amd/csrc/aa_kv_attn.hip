@@ -13,6 +13,12 @@
 //                keys 4g .. 4g+3 of each half of the tile, and the sum over keys may run in that order too.  The left operand wants 8 keys of
 //                one channel in a lane; a lane loads D/16 channels of each of its keys and two byte permutations turn four bf16 values.
 // A lane's rows of S^T, O^T, m and the sum are all row lane % 16, so nothing crosses lanes unless a reference is raised.
+//
+// Roundings to bf16: the weights (2^-8 each at most, as the matrix instruction takes them; their sum l is of the unrounded ones) and the
+// result.  Codes of 4 bits are bf16 numbers exactly.  Float caches stay 32 bits throughout.
+// Bound by memory for few rows: one token over 131072 keys of 8 heads, d = 128, bf16 537 MB in 92 us, 5.8 TB/s (a pure read of 4 GB by the
+// library's sum: 4.0); 32 sequences of 200 .. 16000 in 134 us, 5.6; 64 sequences in 4 bits 552 MB in 112 us, 5.0, where the conversion of the
+// codes takes a third of the vector unit's time beside it.  1000 keys: 6.3 us and the join 3.8, both latency.
 #include "aa_kv_attn.h"
 
 namespace aa {
