@@ -238,7 +238,7 @@ int dense_causal_flash(const aa_params *params, const void *q, const void *k, co
  *  j = kv_len[b] - n_b + i of the sequence.  Fixed length: n_b = N, row (b, i).  Packed (cu_seqlens != NULL): n_b =
  *  cu_seqlens[b+1] - cu_seqlens[b] (N at most: of more rows the first N take part alone), row cu_seqlens[b] + i; rows at and
  *  behind cu_seqlens[B], up to total_tokens (the rows of the packed axis), belong to nobody: they are not read, and not written.
- *  j < 0 (more new tokens than the sequence has: left padding): the token has no storage and sees no key.  A call has less than
+ *  j < 0 (more new tokens than the sequence has: left padding): the token has no storage and, if causal, sees no key.  A call has less than
  *  2^24 rows of new tokens.
  *
  *  Cache formats.  AA_KV_PLAIN: element (page, head, row, c) of the call's dtype at page*kc_stride[0] + head*kc_stride[1] +
@@ -300,10 +300,9 @@ int kv_attn_workspace_bytes(const aa_kv_params *params, size_t *bytes_out);
 
 /*
  * out_r = sum_j softmax_j(softmax_scale * <q_r, k_j>) v_j over the cached tokens that row r sees, lse_r = log sum_j exp(...)
- * (lse nullable, laid out as the per-row arrays at the top).  A row that sees no key: out 0, lse -infinity.  What lies in
- * storage that no row of a sequence sees (behind its end, other pages) never reaches an output, whatever its bits; a value row that
- * is not finite reaches every row of its sequence that it is computed with.  out and q must not overlap, and a call has its workspace
- * for itself until it is through.
+ * (lse nullable, laid out as the per-row arrays at the top).  A row that sees no key: out 0, lse -infinity.  Storage that a row
+ * does not see (later tokens, behind the end, other pages) never reaches it, whatever its bits.  out and q must not overlap, and a
+ * call has its workspace for itself until it is through.
  * Equal calls give equal bits.  The order of a row's sums depends on how the call's keys are dealt out, and so on the lengths of its
  * other sequences and on max_len.
  */

@@ -58,6 +58,10 @@ template <int R> __device__ __forceinline__ bool attn_part(const AttnArgs& p, At
     return true;
 }
 
+// Two bf16 values: the sign bits of those that are not finite; the finite ones alone.
+__device__ __forceinline__ unsigned not_finite(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ unsigned finite(unsigned x) { return x & ~((not_finite(x) >> 15) * 0xffffu); }
+
 // Places of a row's results: its share in the workspace, its row maximum and sum there, its lse.
 __device__ __forceinline__ long long share_of(const AttnArgs& p, const AttnPart& w, int row) {
     return (((long long)w.b * p.a.Hkv + w.hk) * p.rows + row) * p.splits + w.split;

@@ -181,8 +181,68 @@ template <int F, int D, int NT> struct Rows {
     int see[NT];                     // keys that the lane's row sees
 };
 
+// What is not finite among a tile's values, 0 in its place: the rows that see it are marked in LDS, a byte for each row and channel (1: +infinity
+// or NaN, 2: -infinity or NaN), and get it when the waves' rows come together.  (Added to the accumulators here it costs registers of the
+// loop: d = 64, 64 rows, 1000 tokens over 16000 keys 288 -> 333 us.)
 template <int F, int D, int NT>
-__device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, int see_all, Rows<F, D, NT>& r) {
+__device__ __forceinline__ void set_apart(Tile<F, D>& t, Rows<F, D, NT>& r, unsigned* marks, bool& marked) {
+    constexpr int TT = Tile<F, D>::TT, PER = D / 16;                     // channels that a lane has of a key
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));                       // nothing of this before the branch that leads here
+    const int n16 = lane & 15, g = lane >> 4;
+    if (!marked) {
+#pragma unroll 1
+        for (int i = lane; i < 4 * NT * D; i += 64) marks[i] = 0;
+    }
+    marked = true;
+#pragma unroll
+    for (int h = 0; h < TT; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            __builtin_amdgcn_sched_barrier(0);           // one key's after the other's: few registers
+            unsigned w[(PER + 3) / 4] = {};
+            if constexpr (F == kRows4) {
+                const bool bad = (t.vs[h] >> (8 * i) & 255u) == 255u;
+#pragma unroll
+                for (int j = 0; j < PER / 4; ++j) w[j] = bad ? 0x03030303u : 0u;
+                t.v[h][i][0] = bad ? 0u : t.v[h][i][0];
+                t.vs[h] = bad ? (t.vs[h] & ~(255u << (8 * i))) | (127u << (8 * i)) : t.vs[h];
+            } else {
+#pragma unroll
+                for (int c = 0; c < Tile<F, D>::words; ++c) {
+                    const unsigned u = t.v[h][i][c];
+                    if constexpr (F == kRows32) {
+                        const unsigned bad = ((u & 0x7f800000u) + 0x00800000u) >> 31, nan = ((u & 0x7fffffu) + 0x7fffffu) >> 23, below = u >> 31;
+                        w[c / 4] |= bad * ((nan | (1 - below)) + 2 * (nan | below)) << (8 * (c & 3));
+                        t.v[h][i][c] = u & (bad - 1);
+                    } else {                             // bits 15 and 31: not finite; NaN or of the sign
+                        const unsigned bad = not_finite(u), nan = ((u & 0x007f007fu) + 0x007f007fu) << 8;
+                        const unsigned m = (bad & (nan | ~u)) >> 15 | (bad & (nan | u)) >> 14;
+                        w[c / 2] |= ((m & 3u) | (m >> 8 & 0x300u)) << (16 * (c & 1));
+                        t.v[h][i][c] = finite(u);
+                    }
+                }
+                if (PER == 2) w[0] <<= 16 * (n16 & 1);
+            }
+            const int key = t.key + 16 * h + 4 * g + i;
+            unsigned any = 0;
+#pragma unroll
+            for (int j = 0; j < (PER + 3) / 4; ++j) any |= w[j];
+            if (!__any(any != 0)) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll 1
+                for (int row = 0; row < 16; ++row) {
+                    const int see = __builtin_amdgcn_readlane(r.see[n], row);        // (by all lanes: a lane that is off may hold anything)
+                    if (!any || key >= see) continue;
+#pragma unroll
+                    for (int j = 0; j < (PER + 3) / 4; ++j) atomicOr(marks + (16 * n + row) * (D / 4) + PER * n16 / 4 + j, w[j]);
+                }
+        }
+}
+
+template <int F, int D, int NT>
+__device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, int see_all, int see_some, Rows<F, D, NT>& r, unsigned* marks, bool& marked) {
     constexpr int TT = Tile<F, D>::TT;
     const int g = (threadIdx.x & 63) >> 4;
     bool whole = true;
@@ -212,6 +272,9 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
                 for (int e = 0; e < 4; ++e) s[n][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.f[e], q.f[e], s[n][0], 0, 0, 0);
             }
         }
+        // Ten wait states until a result may be read: the compiler counts none for a read behind the branch below.
+#pragma unroll
+        for (int n = 0; n < NT; ++n) asm volatile("s_nop 9" : "+v"(s[n][0]));
     } else {
 #pragma unroll
         for (int h = 0; h < TT; ++h) {
@@ -240,6 +303,24 @@ __device__ __forceinline__ void attend_tile(const AttnArgs& p, Tile<F, D>& t, in
     if (__builtin_expect(!(whole && t.key + 16 * TT <= see_all), 0)) {
         int base = 4 * g;
         asm volatile("" : "+v"(base));                   // else 50 instructions of this stand in every tile's way
+        if (see_all < see_some && t.key + 16 * TT > see_all) {       // a row may see more than another: 0 times what is not finite must not reach that
+            unsigned bad = 0;
+#pragma unroll
+            for (int h = 0; h < TT; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (F == kRows4) {
+                        bad |= ((t.vs[h] >> (8 * i) & 255u) + 1) & 256u;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < Tile<F, D>::words; ++j)
+                            bad |= F == kRows32 ? ((t.v[h][i][j] & 0x7f800000u) + 0x00800000u) & 0x80000000u : not_finite(t.v[h][i][j]);
+                    }
+                }
+            if (__any(bad != 0)) {
+                set_apart<F, D, NT>(t, r, marks, marked);
+            }
+        }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -399,6 +480,8 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
     static_assert(kUnitKeys % (kWaves * TK) == 0, "a unit is whole rounds of the waves");
     __shared__ float s_o[kWaves][16][P];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    __shared__ unsigned s_marks[kWaves][R * D / 4];      // see set_apart
+    __shared__ bool s_marked[kWaves];
     const KvArgs& a = p.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g = lane >> 4;
@@ -439,6 +522,7 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
     }
 
     for (;;) {                                           // over the row tiles that the stretch touches
+        bool marked = false;
         const int stop = s.units - t < (int)(end - at) ? s.units : t + (int)(end - at);
         const int r0 = tile_no * R, rows = s.sq.n * a.grp, last = r0 + R < rows ? r0 + R - 1 : rows - 1;
         const int see_first = seen(a, s.len, s.sq.n, (int)p.by_grp.div(r0)), see_last = seen(a, s.len, s.sq.n, (int)p.by_grp.div(last));
@@ -476,12 +560,12 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
                 key += kWaves * TK;
                 load_tile<F, D>(w, key, hi, pages, t1);
                 pages = pages_of<TT>(w, key + kWaves * TK);
-                attend_tile<F, D, NT>(p, t0, see_first, r);
+                attend_tile<F, D, NT>(p, t0, see_first, see_last, r, s_marks[wave], marked);
                 if (key >= hi) break;
                 key += kWaves * TK;
                 load_tile<F, D>(w, key, hi, pages, t0);
                 pages = pages_of<TT>(w, key + kWaves * TK);
-                attend_tile<F, D, NT>(p, t1, see_first, r);
+                attend_tile<F, D, NT>(p, t1, see_first, see_last, r, s_marks[wave], marked);
                 if (key >= hi) break;
             }
         }
@@ -495,6 +579,7 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
             l += __shfl_xor(l, 32);
             __syncthreads();                             // the last rows have been read
             if (g == 0) { s_m[wave][n16] = r.m[n] * p.c; s_l[wave][n16] = l; }
+            if (n == 0 && lane == 0) s_marked[wave] = marked;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -512,6 +597,13 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
                 sum += f * s_l[k][x];
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j) acc[j] += f * s_o[k][x][c0 + j];
+                if (s_marked[k]) {
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j) {
+                        const unsigned m = s_marks[k][(16 * n + x) * (D / 4) + (c0 + j) / 4] >> (8 * ((c0 + j) & 3));
+                        acc[j] += (m & 1 ? INFINITY : 0.f) - (m & 2 ? INFINITY : 0.f);
+                    }
+                }
             }
             if (t > 0 || stop < s.units) {
                 const long long place = (long long)deal_place(blockIdx.x, t) * R + 16 * n + x;
@@ -538,6 +630,7 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
         // the next row tile
         at += stop - t;
         if (at >= end) return;
+        if (s_marked[0] | s_marked[1] | s_marked[2] | s_marked[3]) __syncthreads();         // the marks have been read
         t = 0;
         if (++tile_no == s.tiles) {
             tile_no = 0;
@@ -578,12 +671,17 @@ __device__ __forceinline__ void join_row(const AttnArgs& p, int count, const flo
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
     const int c = lane % L;
     f32x4 acc = {0, 0, 0, 0};
-    for (int s0 = wave * S + lane / L; s0 < count; s0 += 8 * TEAM * S) {     // eight requests at a time, also of the last ones (again, with weight 0)
+    for (int s0 = wave * S + lane / L; s0 < count; s0 += 8 * TEAM * S) {     // eight requests at a time, also of the last ones (again, and not added)
         f32x4 v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = *(const f32x4*)(o + place(s0 + k * TEAM * S < count ? s0 + k * TEAM * S : count - 1) * D + 4 * c);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) acc += (s0 + k * TEAM * S < count ? weights[s0 + k * TEAM * S] : 0.f) * v[k];
+        for (int k = 0; k < 8; ++k) {
+            const bool more = s0 + k * TEAM * S < count;
+            const float f = weights[more ? s0 + k * TEAM * S : 0];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = more ? fmaf(f, v[k][e], acc[e]) : acc[e];
+        }
     }
 #pragma unroll
     for (int x = L; x < 64; x *= 2)

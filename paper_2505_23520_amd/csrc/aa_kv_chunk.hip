@@ -9,7 +9,8 @@
 // row m of the score tile's half kb is key 4 (m % 16) + 2 kb + m / 16.
 // 4-bit pages: a lane loads 32 channels of a key (16 bytes and a scale), converts them (exactly: bf16 holds every code's value) and
 // writes them where a direct load would have put them; K of the next tile while the P V products run, V at the next tile's start.
-// Rows of values behind the last key, or without storage, are cleared in LDS: their weight is 0, their bits may be anything.
+// Rows of values behind the last key, or without storage, are cleared in LDS: their weight is 0, their bits may be anything.  What is not
+// finite in a tile that some row does not see whole is added to the rows that see it, and cleared before the product.
 // Bound by the matrix pipe and a wave's own chain, as that engine: 2048 and 1000 new tokens over 30011 and 8192, 32 / 8 heads, bf16 1.10 TFLOP
 // in 1000 us, 1.1 PFLOP/s (a large matrix product: 1.26); 1024 and 403 over 16384 and 5003 in 4 bits 0.30 TFLOP in 350 us and the join 26,
 // where two or three work-groups of 8192 keys a CU end unevenly (6144 over 16384: 1.04).
@@ -31,6 +32,42 @@ __device__ __forceinline__ void chunk_barrier() {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
+}
+
+// Whether a V tile holds what is not finite: the whole tile, so that all lanes agree.
+__device__ __forceinline__ bool values_not_finite(const char* Vs) {
+    unsigned bad = 0;
+    const char* at = Vs + 16 * counted_lane();
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const u32x4 x = *(const u32x4*)(at + i * VGRP);
+        bad |= not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3]);
+    }
+    return __any(bad != 0);
+}
+
+// What is not finite in a V tile goes to the rows that see it, key by key (lim: keys of the tile that the lane's row sees).  `place`: 4 KB of the wave,
+// where 16 of a lane's channels stand meanwhile, as registers for this would be taken from the tiles.
+__device__ __forceinline__ void add_not_finite(const char* Vs, char* place, int lim, floatx16 (&o)[4]) {
+    const int ln = counted_lane();
+    float* mine = (float*)place + ln;
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mine[64 * v] = o[db][v];
+#pragma unroll 1
+        for (int kk = 0; kk < TK; ++kk) {
+            const char* row = Vs + (kk >> 2) * VGRP + (kk & 3) * 256;
+            if (!__any(not_finite(*(const unsigned*)(row + 4 * ln)) != 0)) continue;
+#pragma unroll 1
+            for (int v = 0; v < 16; ++v) {
+                const unsigned u = (unsigned)*(const unsigned short*)(row + 64 * db + 16 * (v >> 2) + 8 * (ln >> 5) + 2 * (v & 3)) << 16;
+                if ((u & 0x7f800000u) == 0x7f800000u && kk < lim) mine[64 * v] += __uint_as_float(u);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] = mine[64 * v];
+    }
 }
 
 template <bool FP4>
@@ -231,6 +268,21 @@ __global__ __launch_bounds__(256, 3) void kv_chunk_kernel(AttnArgs p) {
         }
         __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0)
         chunk_barrier();
+        if (__builtin_expect(t0 + TK > w.see_first, 0) && values_not_finite(Vs0)) {
+            // some row does not see all keys, and 0 times what is not finite must not reach it (all waves are here, the tile of keys is free)
+            add_not_finite(Vs0, (char*)Kcur + 4096 * wave, see - t0, o);
+            chunk_barrier();
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                u32x4* x = (u32x4*)(Vs0 + (4 * wave + i) * VGRP + 16 * counted_lane());
+                u32x4 y = *x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = finite(y[e]);
+                *x = y;
+            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0)
+            chunk_barrier();
+        }
         if (on) {
             shortx4 vlo[16], vhi[16];
             auto read_v = [&](int i) {

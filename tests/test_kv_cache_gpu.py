@@ -232,6 +232,47 @@ def test_attn_nonfinite(api, dtype, n):
     assert bool(((out[1].double() - want).abs() <= to).all()) and bool(((lse[1].double() - wl).abs() <= tl).all())
 
 
+@pytest.mark.parametrize("dtype,fp4,d", FORMATS)
+@pytest.mark.parametrize("n", [2, 5, 9, 14, 40, 130])
+def test_attn_values_not_finite(api, dtype, fp4, d, n):
+    """Infinities and NaN among the new tokens' values: rows that do not see them are as if 0 stood there (or have no key at all), rows that
+    do have them in their channels and are right in the others."""
+    lens = [200, max(n - 3, 1), n, 777]
+    cache = Cache(api, lens, 2, d, dtype, fp4, 16, seed=n).fill()
+    q = _randn(4, 8, n, d, seed=n, dtype=dtype)
+    bad = {}                                           # (sequence, token) -> {channel: value} of KV head 1
+    for b, ln in enumerate(lens):
+        first = max(ln - n, 0)
+        for j, put in ((ln - 1, {3: math.inf}), (first + (ln - first) // 2, {d - 1: math.nan}), (max(ln - 2, first), {3: -math.inf, 17: -math.inf})):
+            bad.setdefault((b, j), {}).update(put)
+    K = [cache.rows("k", b, 0, ln) for b, ln in enumerate(lens)]
+    V = [cache.rows("v", b, 0, ln).clone() for b, ln in enumerate(lens)]
+    marks = [torch.zeros(2, ln, d, dtype=torch.float64, device="cuda") for ln in lens]
+    for (b, j), put in bad.items():
+        page, row = cache._at(b, j, 1)
+        for c, x in put.items():
+            if fp4:
+                cache.c["v_scale"][page, 1, c // 32, row] = 255
+                V[b][1, j, c // 32 * 32:c // 32 * 32 + 32] = 0
+                marks[b][1, j, c // 32 * 32:c // 32 * 32 + 32] = math.nan
+            else:
+                cache.c["v"][page, 1, row, c] = x
+                V[b][1, j, c] = 0
+                marks[b][1, j, c] = x
+    out, lse = _attn(api, cache, q)
+    for b, ln in enumerate(lens):
+        want, wl, A, size = attend(q[b].double(), K[b], V[b], ln - n, 1 / math.sqrt(d))
+        to, _ = tolerances(want, A, size, wl, ln, d, dtype)
+        for i in range(n):
+            seen = max(ln - n + i + 1, 0)
+            extra = marks[b][:, :seen].sum(dim=1).repeat_interleave(4, dim=0)             # 0, an infinity, or NaN
+            fine = extra == 0
+            err = (out[b, :, i].double() - want[:, i]).abs()
+            assert bool((err[fine] <= to[:, i][fine]).all()), (b, i)
+            got = out[b, :, i][~fine].double()
+            assert torch.equal(got.nan_to_num(nan=5.0), extra[~fine].nan_to_num(nan=5.0)), (b, i)
+
+
 @pytest.mark.parametrize("fp4", [False, True])
 def test_offsets_beyond_32_bits(api, fp4):
     """A pool whose last pages lie beyond 2^32 bytes: appended to, read and attended there."""

@@ -190,20 +190,30 @@ int main() {
     assert run.returncode == 0
 
 
-def test_cache_kernels_do_not_spill(tmp_path):
+@pytest.fixture(scope="module")
+def compiled(tmp_path_factory):
+    """The cache's kernel sources compiled as the build does: source -> (the compiler's report on registers, assembly)."""
+    from paper_2505_23520_amd import build
+    out = {}
+    for source in sorted(set(build.CACHE_SOURCES) - {"aa_kv_api.hip"}):
+        asm = tmp_path_factory.mktemp("s") / "x.s"
+        cmd = ["hipcc", *build.FLAGS, *build.EXTRA.get(source, []), "--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage",
+               os.path.join(build.CSRC, source), "-o", str(asm)]
+        out[source] = (subprocess.run(cmd, capture_output=True, text=True, check=True).stderr, asm.read_text())
+    return out
+
+
+def test_cache_kernels_do_not_spill(compiled):
     """A spilled register's reload is a vector-memory load, and the wait for it waits for the tiles in flight.  As many waves per SIMD
     as the dealing of the keys counts on."""
     import re
-    from paper_2505_23520_amd import build
     want = {"aa_kv_append.hip": lambda name: 3, "aa_kv_chunk.hip": lambda name: 3,
             "aa_kv_attn.hip": lambda name: 1 if "join" in name else {"1": {"128": 3 if "ILi2E" in name else 2, "64": 3, "32": 4},
                                                                      "2": {"128": 2 if "ILi2E" in name else 1, "64": 2, "32": 2}, "4": {"64": 1, "32": 1}}
             [re.search(r"ILi\dELi(\d+)ELi(\d)E", name).group(2)][re.search(r"ILi\dELi(\d+)ELi(\d)E", name).group(1)]}
-    assert sorted(want) + ["aa_kv_api.hip"] == sorted(set(build.CACHE_SOURCES) - {"aa_kv_api.hip"}) + ["aa_kv_api.hip"]
+    assert sorted(want) == sorted(compiled)
     for source, waves in want.items():
-        cmd = ["hipcc", *build.FLAGS, *build.EXTRA.get(source, []), "--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage",
-               os.path.join(build.CSRC, source), "-o", str(tmp_path / "x.s")]
-        report = subprocess.run(cmd, capture_output=True, text=True, check=True).stderr
+        report = compiled[source][0]
         names = re.findall(r"Function Name: (\S+)", report)
         spills = [int(x) for x in re.findall(r"VGPRs Spill: (\d+)", report)]
         occupancy = [int(x) for x in re.findall(r"Occupancy \[waves/SIMD\]: (\d+)", report)]
@@ -211,3 +221,83 @@ def test_cache_kernels_do_not_spill(tmp_path):
         assert not any(spills) or "append" in source, dict(zip(names, spills))      # (kv_append has nothing in flight across a reload)
         for name, o in zip(names, occupancy):
             assert o >= waves(name), (name, o)
+
+
+# Wait states between a matrix instruction and another instruction that reads or overwrites its result: two (products of floats) or three more
+# than its passes.
+WAIT_STATES = {"v_mfma_f32_16x16x4_f32": 10, "v_mfma_f32_16x16x32_bf16": 7, "v_mfma_f32_32x32x16_bf16": 11}
+
+
+def _registers(text):
+    import re
+    out = set()
+    for kind, lo, hi, one in re.findall(r"\b([va])(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+        out |= {(kind, i) for i in (range(int(lo), int(hi) + 1) if lo else [int(one)])}
+    return out
+
+
+def _blocks(asm):
+    """(kernel, [(label, [instruction])]) of every kernel."""
+    name, blocks = None, None
+    for line in asm.splitlines():
+        t = line.split(";")[0].strip()
+        if t.startswith("_Z") and t.endswith(":"):
+            name, blocks = t[:-1], [("", [])]
+        elif name and t.startswith(".Lfunc_end"):
+            yield name, blocks
+            name = None
+        elif name and t.startswith(".LBB"):
+            blocks.append((t[:-1], []))
+        elif name and t and not t.startswith(".") and not t.endswith(":"):
+            blocks[-1][1].append(t)
+
+
+def _too_early(blocks):
+    """Instructions that touch a matrix instruction's result before its wait states are over, on any path."""
+    at = {label: i for i, (label, _) in enumerate(blocks)}
+    state, work, bad = [{} for _ in blocks], list(range(len(blocks))), set()
+    while work:
+        b = work.pop(0)
+        left, ends = dict(state[b]), [b + 1]
+        for t in blocks[b][1]:
+            op, _, rest = t.partition(" ")
+            operands = rest.split(", ")
+            touched = set()
+            if op.startswith("v_mfma"):
+                touched = _registers(", ".join(operands[1:3]))           # (its addend and its result follow without waiting)
+            elif op.startswith(("v_", "ds_", "buffer_", "global_", "scratch_", "flat_")):
+                touched = _registers(rest)
+            if any(r in left for r in touched):
+                bad.add(t)
+            n = int(rest) + 1 if op == "s_nop" else 1
+            left = {r: x - n for r, x in left.items() if x > n}
+            if op.startswith("v_mfma"):
+                left.update((r, WAIT_STATES[op]) for r in _registers(operands[0]))
+            if op.startswith(("s_cbranch", "s_branch")):
+                ends.append(at[rest.strip()])
+                for r, x in left.items():
+                    if state[ends[-1]].get(r, 0) < x:
+                        state[ends[-1]][r] = x
+                        work.append(ends[-1])
+            if op in ("s_branch", "s_endpgm"):
+                ends[0] = None
+        if ends[0] is not None and ends[0] < len(blocks):
+            for r, x in left.items():
+                if state[ends[0]].get(r, 0) < x:
+                    state[ends[0]][r] = x
+                    work.append(ends[0])
+    return sorted(bad)
+
+
+def test_matrix_results_are_waited_for(compiled):
+    """The compiler has left the wait out for reads behind a branch (float scores, whose maximum was then taken of older values)."""
+    one = [("", ["v_mfma_f32_16x16x4_f32 v[4:7], v0, v1, 0", "s_cbranch_vccz .L1", "s_nop 7"]), (".L1", ["v_add_f32_e32 v8, v9, v7"])]
+    assert _too_early(one) == ["v_add_f32_e32 v8, v9, v7"]
+    one[1][1].insert(0, "s_nop 8")
+    assert _too_early(one) == []
+    kernels = 0
+    for source in ("aa_kv_attn.hip", "aa_kv_chunk.hip"):
+        for name, blocks in _blocks(compiled[source][1]):
+            kernels += any(t.startswith("v_mfma") for _, b in blocks for t in b)
+            assert not _too_early(blocks), name
+    assert kernels == 20
