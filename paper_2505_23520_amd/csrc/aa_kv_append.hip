@@ -102,9 +102,13 @@ __device__ __forceinline__ Token token_of(const KvArgs& a, long long row) {
     if (!a.cu) {
         t.b = (int)(row / a.N);
     } else {
-        for (int at = 0; at < a.B; at += 64) {      // sequences that end at or before the row
-            const int i = at + (threadIdx.x & 63);
-            t.b += __popcll(__ballot(i < a.B && a.cu[i + 1] <= row));
+        // sequences that end at or before the row: 64 of them looked at at once, then those between two of them (1024 sequences of a token
+        // 8.3 us, and 12.2 with all of them looked at)
+        for (int step = a.B; step > 1;) {
+            const int end = t.b + step < a.B ? t.b + step : a.B;
+            step = (step + 63) / 64;
+            const int i = t.b + ((int)(threadIdx.x & 63) + 1) * step;
+            t.b += step * __popcll(__ballot(i <= end && a.cu[i] <= row));
         }
     }
     t.i = -1;

@@ -416,6 +416,28 @@ def test_append_packed_with_positions(api, dtype, fp4):
         at += m
 
 
+@pytest.mark.parametrize("B", [65, 200, 4097, 5000])
+def test_append_packed_many_sequences(api, B):
+    """Which sequence a packed row belongs to, many of them without rows: each row stored at its sequence's end, and read back."""
+    gen = torch.Generator().manual_seed(B)
+    new = torch.randint(0, 4, (B,), generator=gen)
+    new[torch.rand(B, generator=gen) < 0.3] = 0
+    lens = (new + torch.randint(0, 9, (B,), generator=gen)).tolist()
+    T, d = int(new.sum()), 64
+    cache = Cache(api, lens, 1, d, BF, False, 16, seed=1)
+    k, v = (_randn(1, T + 2, d, seed=s) for s in (1, 2))
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)]).int().cuda()
+    _append(api, cache, None, k, v, 0, cu=cu, max_new=3)
+    b = torch.repeat_interleave(torch.arange(B), new)
+    j = torch.tensor(lens)[b] - new[b] + torch.arange(T) - cu[:-1].cpu()[b]
+    page = cache.table.cpu()[b, 0].long().cuda()
+    assert torch.equal(cache.c["k"][page, 0, j.cuda()], k[0, :T]) and torch.equal(cache.c["v"][page, 0, j.cuda()], v[0, :T])
+    assert int((~torch.isnan(cache.c["k"][..., 0])).sum()) == T
+    ko, vo = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    api.kv_read(api.make_kv_params(cache.c, cache.table, cache.kv_len, k=ko, v=vo, cu_seqlens=cu, max_new=3), ko, vo)
+    assert torch.equal(ko[:, :T], k[:, :T]) and torch.equal(vo[:, :T], v[:, :T]) and torch.all(ko[:, T:] == 7.0)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_append_in_place_and_parts(api, dtype):
     """q_out == q and k_out == k; queries alone; keys and values alone; no k_out."""
