@@ -53,7 +53,7 @@ int launch_kv_read(const KvArgs& a, int dtype, int format, int d, void* k_out, v
 
 // How kv_attn deals the keys out (see AttnArgs), and the workspace that takes.  longest: of the sequences, as far as the caller knows; room:
 // what a sequence can have at most.
-struct KvSplit { int groups, splits, chunk, whole; size_t ws_bytes; };
+struct KvSplit { int groups, splits, whole; size_t ws_bytes; };
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room);
 int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit& sp, const void* q, void* out, float* lse, float* ws,
                    hipStream_t st);

@@ -13,7 +13,7 @@ struct AttnArgs {
     int rows, tiles;                 // most rows of a KV head and sequence (N * grp), their row tiles
     int groups, whole;               // registers: work-groups that the line of units is dealt to; whole: a tile is one unit, however long
     int tell;                        // registers: the work-groups tell the joining kernel which tiles are shared
-    int splits, chunk;               // LDS: work-groups of a row tile, keys of each (the last one's: what is left)
+    int splits;                      // LDS: work-groups of a row tile
     float c;                         // sigma * log2 e
     float slack;                     // a reference is raised when a score exceeds it by this much: weights stay below 2^8
     FastDiv by_hkv, by_splits, by_grp, by_groups;
@@ -30,6 +30,12 @@ __device__ __forceinline__ int seen(const KvArgs& a, int len, int n, int i) {
     long long x = a.causal ? (long long)len - n + i + 1 : len;
     if (x > room) x = room;
     return x < 0 ? 0 : (int)x;
+}
+
+// Keys of a share in the kernel through LDS (the last one's: what is left): every sequence's keys in as many shares, but no small ones.
+__device__ __forceinline__ int share_keys(const AttnArgs& p, int len, int n) {
+    const int all = seen(p.a, len, n, n - 1), keys = ((int)p.by_splits.div(all + p.splits - 1) + 127) & ~127;
+    return keys < 256 ? 256 : keys;
 }
 
 // A work-group's rows and keys.  KV heads are dealt out first (to one XCD each where there are eight of them: its L2 then serves all row
@@ -52,9 +58,10 @@ template <int R> __device__ __forceinline__ bool attn_part(const AttnArgs& p, At
     w.last = w.r0 + R < w.rows ? w.r0 + R - 1 : w.rows - 1;
     const int see_last = seen(a, w.len, w.sq.n, (int)p.by_grp.div(w.last));
     w.see_first = seen(a, w.len, w.sq.n, (int)p.by_grp.div(w.r0));
-    w.lo = w.split * p.chunk;
+    const int keys = share_keys(p, w.len, w.sq.n);
+    w.lo = w.split * keys;
     if (w.split && w.lo >= see_last) return false;
-    w.hi = w.split == p.splits - 1 || see_last - w.lo < p.chunk ? see_last : w.lo + p.chunk;
+    w.hi = w.split == p.splits - 1 || see_last - w.lo < keys ? see_last : w.lo + keys;
     return true;
 }
 

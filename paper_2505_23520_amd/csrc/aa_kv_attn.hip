@@ -711,7 +711,8 @@ __global__ __launch_bounds__(256) void kv_join_rows_kernel(AttnArgs p) {
     const int i = (int)p.by_grp.div(row), h = hk * a.grp + row - i * a.grp;
     if (i >= sq.n) return;
     // a share wrote this row if its keys begin before those that the row's tile of rows sees end; before those of the row is enough
-    int parts = (int)(((long long)seen(a, a.kv_len[b], sq.n, i) + p.chunk - 1) / p.chunk);
+    const int len = a.kv_len[b], keys = share_keys(p, len, sq.n);
+    int parts = (seen(a, len, sq.n, i) + keys - 1) / keys;
     parts = parts > p.splits ? p.splits : parts < 1 ? 1 : parts;
     const long long at = (((long long)b * a.Hkv + hk) * p.rows + row) * p.splits;
     const float* ml = share_sums(p, D);
@@ -806,7 +807,7 @@ constexpr int kCUs = 256;
 KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room) {
     const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype, format), tiles = (rows + R - 1) / R;
     const long long items = tiles * B * Hkv;
-    KvSplit s = {0, 1, 0, 0, 0};
+    KvSplit s = {0, 1, 0, 0};
     if (R < kChunkRows) {
         // as many work-groups as run at once, or as there are units
         const int o = dtype == 0 ? (d == 32 ? occupancy<kRows32, 32>(R) : d == 64 ? occupancy<kRows32, 64>(R) : occupancy<kRows32, 128>(R))
@@ -837,9 +838,7 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
     for (long long n = splits, most = 2 * splits + 2; n <= most && n * 512 <= longest; ++n)
         if (cost(n) < cost(splits)) splits = n;
     if (splits > kMaxShares) splits = kMaxShares;
-    const long long chunk = ((longest + splits - 1) / splits + 127) / 128 * 128;
-    s.splits = (int)((longest + chunk - 1) / chunk);
-    s.chunk = (int)chunk;
+    s.splits = (int)splits;
     if (s.splits > 1) s.ws_bytes = (size_t)B * Hkv * rows * s.splits * (d + 2) * 4;
     return s;
 }
@@ -850,7 +849,7 @@ int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit&
     p.a = a;
     p.q = q; p.out = out; p.lse = lse;
     p.ws = sp.ws_bytes ? ws : nullptr;
-    p.groups = sp.groups; p.whole = sp.whole; p.splits = sp.splits; p.chunk = sp.chunk;
+    p.groups = sp.groups; p.whole = sp.whole; p.splits = sp.splits;
     p.rows = a.N * a.grp;
     const int R = tile_rows(p.rows, d, dtype, format);
     p.tiles = (p.rows + R - 1) / R;
