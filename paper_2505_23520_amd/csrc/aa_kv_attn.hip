@@ -643,17 +643,25 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
     }
 }
 
-// The shares of a row together, a wave a row or (TEAM = 4) a work-group a row: first their maxima and sums, a share a lane, which leave a
-// weight for each in LDS; then D / 4 lanes a share, 16 bytes of its row each, 256 / D shares a wave at once and eight times as many on
-// their way.
+// The shares of a row together, a wave a row or (TEAM = 4) a work-group a row: their maxima and sums, a share a lane, leave a weight for
+// each in LDS; D / 4 lanes take a share, 16 bytes of its row each, 256 / D shares a wave at once and two or eight (BATCH) times as many on
+// their way, the first of them before the weights are known (1000 keys: 9.8 -> 9.2 us with the kernel before).
 // place(s): where share s stands; o, ml: the first place's values, and maximum and sum.
 // mine: maximum and sum of share `lane`, requested ahead (of a share beyond count: anything).
 constexpr int kMaxShares = 1024;
-template <class T, int D, int TEAM, class Place>
-__device__ __forceinline__ void join_row(const AttnArgs& p, int count, const float* o, const float* ml, Place place, f32x2 mine,
+template <class T, int D, int TEAM, int BATCH, class Place>
+__device__ __forceinline__ void join_batches(const AttnArgs& p, int count, const float* o, const float* ml, Place place, f32x2 mine,
                                          float* weights, f32x4* part, T* out, float* lse) {
     constexpr int L = D / 4, S = 64 / L;
-    const int lane = threadIdx.x & 63, wave = TEAM == 1 ? 0 : threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = TEAM == 1 ? 0 : threadIdx.x >> 6, c = lane % L;
+    // a batch's requests at a time, also of the last ones (again, and not added); the first before the weights are known
+    f32x4 v[BATCH];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) v[k] = *(const f32x4*)(o + place(s0 + k * TEAM * S < count ? s0 + k * TEAM * S : count - 1) * D + 4 * c);
+    };
+    int s0 = wave * S + lane / L;
+    load(s0);
     if (lane >= count) mine = f32x2{-INFINITY, 0.f};
     float m = mine[0];
     for (int s = lane + 64; s < count; s += 64) m = fmaxf(m, ml[2 * place(s)]);
@@ -669,19 +677,18 @@ __device__ __forceinline__ void join_row(const AttnArgs& p, int count, const flo
     }
 #pragma unroll
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    const int c = lane % L;
     f32x4 acc = {0, 0, 0, 0};
-    for (int s0 = wave * S + lane / L; s0 < count; s0 += 8 * TEAM * S) {     // eight requests at a time, also of the last ones (again, and not added)
-        f32x4 v[8];
+    for (;;) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = *(const f32x4*)(o + place(s0 + k * TEAM * S < count ? s0 + k * TEAM * S : count - 1) * D + 4 * c);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < BATCH; ++k) {
             const bool more = s0 + k * TEAM * S < count;
             const float f = weights[more ? s0 + k * TEAM * S : 0];
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] = more ? fmaf(f, v[k][e], acc[e]) : acc[e];
         }
+        s0 += BATCH * TEAM * S;
+        if (s0 >= count) break;
+        load(s0);
     }
 #pragma unroll
     for (int x = L; x < 64; x *= 2)
@@ -698,6 +705,13 @@ __device__ __forceinline__ void join_row(const AttnArgs& p, int count, const flo
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[4 * c + e] = (T)(l == 0.f ? 0.f : acc[e] / l);
     if (lse && c == 0) *lse = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+}
+
+template <class T, int D, int TEAM, class Place>
+__device__ __forceinline__ void join_row(const AttnArgs& p, int count, const float* o, const float* ml, Place place, f32x2 mine,
+                                         float* weights, f32x4* part, T* out, float* lse) {
+    if (count <= 2 * TEAM * (256 / D)) join_batches<T, D, TEAM, 2>(p, count, o, ml, place, mine, weights, part, out, lse);
+    else join_batches<T, D, TEAM, 8>(p, count, o, ml, place, mine, weights, part, out, lse);
 }
 
 // The chunk kernel's shares, which stand row by row: a work-group for four rows of a KV head.
@@ -828,8 +842,8 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
     // the others, 2048 and 1000 new tokens over 30011 and 8192 took 1148 us instead of 996).  Keys are split until there are as
     // many work-groups as run at once, three a CU, or shares of 256 keys, and up to twice as often where the fullest CU then has
     // less to do: a CU takes 16.5 us for 1000 keys of a tile however many work-groups bring them, a share of 128 rows 0.027 us of the
-    // chip's memory time.  32 / 8 heads, 2 / 3 / 4 / 6 shares: 2 x 800 over 20000 keys 678 / 534 / 578 / 557 us; 1024 and 403 over 16384 and
-    // 5003 in 4 bits 369 / 382 / 433 / 382 (1: 529).
+    // chip's memory time.  32 / 8 heads, 1 / 2 / 3 / 4 / 6 shares: 2 x 800 tokens over 20000 keys 559 / 671 / 563 / 590 / 574 us; 512 over 32768
+    // 754 / 423 / 322 / 290 / 288; 1024 and 403 over 16384 and 5003 in 4 bits 496 / 382 / 379 / 383 / 386.
     long long splits = (kCUs * 3 + items - 1) / items;
     if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
     auto cost = [&](long long n) {
