@@ -18,7 +18,7 @@
 // result.  Codes of 4 bits are bf16 numbers exactly.  Float caches stay 32 bits throughout.
 // Bound by memory for few rows: one token over 131072 keys of 8 heads, d = 128, bf16 537 MB in 92 us, 5.8 TB/s (a pure read of 4 GB by the
 // library's sum: 4.0); 32 sequences of 200 .. 16000 in 134 us, 5.6; 64 sequences in 4 bits 552 MB in 112 us, 5.0, where the conversion of the
-// codes takes a third of the vector unit's time beside it.  1000 keys: 6.3 us and the join 3.8, both latency.
+// codes takes a third of the vector unit's time beside it.  1000 keys: 6.3 us and the join 3, both latency.
 #include "aa_kv_attn.h"
 
 namespace aa {
@@ -635,8 +635,8 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
         if (++tile_no == s.tiles) {
             tile_no = 0;
             int b = s.b;
-            do {                                         // (ends: units are left)
-                if (++b == a.B) { b = 0; ++hk; }
+            do {                                         // (units are left; if lengths change under a call it ends here)
+                if (++b == a.B) { b = 0; if (++hk == a.Hkv) return; }
                 s = part_of<R>(p, b);
             } while (s.units == 0);
         }
