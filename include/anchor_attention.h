@@ -235,11 +235,12 @@ int dense_causal_flash(const aa_params *params, const void *q, const void *k, co
  *  nothing is attended, and kv_read gives zeros.  Sequences may share pages that nobody appends to.
  *
  *  New tokens.  kv_len[b] counts the tokens of sequence b INCLUDING the call's n_b new ones: new token i is token
- *  j = kv_len[b] - n_b + i of the sequence.  Fixed length: n_b = N, row (b, i).  Packed (cu_seqlens != NULL): n_b =
+ *  j = kv_len[b] - n_b + i of the sequence.  Fixed length: n_b = N, row (b, i).  Packed (cu_seqlens != NULL, ascending): n_b =
  *  cu_seqlens[b+1] - cu_seqlens[b] (N at most: of more rows the first N take part alone), row cu_seqlens[b] + i; rows at and
  *  behind cu_seqlens[B], up to total_tokens (the rows of the packed axis), belong to nobody: they are not read, and not written.
  *  j < 0 (more new tokens than the sequence has: left padding): the token has no storage and, if causal, sees no key.  A call has less than
- *  2^24 rows of new tokens.
+ *  2^24 rows of new tokens (B*N, or total_tokens).  kv_attn takes every such call with N*Hq < 2^30, rows*Hq < 2^34 and B*Hkv < 2^30; beyond,
+ *  its tiles of rows may be more than 32 bits count, and the call AA_EUNSUPPORTED.
  *
  *  Cache formats.  AA_KV_PLAIN: element (page, head, row, c) of the call's dtype at page*kc_stride[0] + head*kc_stride[1] +
  *  row*kc_stride[2] + c; strides in elements, multiples of 16 bytes.

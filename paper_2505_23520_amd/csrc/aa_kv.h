@@ -51,10 +51,10 @@ int launch_kv_append(const KvArgs& a, int dtype, int format, int d, const void* 
                      const float* inv_freq, const int* positions, void* q_out, void* k_out, hipStream_t st);
 int launch_kv_read(const KvArgs& a, int dtype, int format, int d, void* k_out, void* v_out, hipStream_t st);
 
-// How kv_attn deals the keys out (see AttnArgs), and the workspace that takes.  longest: of the sequences, as far as the caller knows; room:
-// what a sequence can have at most.
-struct KvSplit { int groups, splits, whole; size_t ws_bytes; };
-KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room);
+// How kv_attn deals the keys out (see AttnArgs), and the workspace that takes.  total: rows of the token axis; longest: of the sequences, as far
+// as the caller knows; room: what a sequence can have at most.  fits: the kernels can count the call's work in 32 bits.
+struct KvSplit { int groups, splits, whole; size_t ws_bytes; bool fits; };
+KvSplit kv_split(int B, int Hq, int Hkv, int N, long long total, int d, int dtype, int format, long long longest, long long room);
 int launch_kv_attn(const KvArgs& a, int dtype, int format, int d, const KvSplit& sp, const void* q, void* out, float* lse, float* ws,
                    hipStream_t st);
 

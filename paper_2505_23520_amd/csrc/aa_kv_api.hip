@@ -58,11 +58,8 @@ int make_args(const aa_kv_params* p, KvArgs* a) {
     if ((int64_t)p->max_pages * p->page_size > (1 << 30)) return AA_EUNSUPPORTED;       // tokens of a sequence are counted in 32 bits
     // sequences stand on y of a launch grid, a work-group of 256 threads for every token on x, whose threads are counted in 32 bits
     if (p->B > 65535 || p->Hq > 65535) return AA_EUNSUPPORTED;
-    // units of all rows (see aa_kv_deal.h) are counted in 32 bits
-    if ((int64_t)p->B * p->Hkv > (1ll << 31) / ((int64_t)p->max_pages * p->page_size / 128 + 1) / (((int64_t)p->N * (p->Hq / p->Hkv) + 15) / 16 + 1))
-        return AA_EUNSUPPORTED;
     const int64_t tokens = p->cu_seqlens ? p->total_tokens : (int64_t)p->B * p->N;
-    if (tokens >= (1 << 24) || (int64_t)p->N * (p->Hq / p->Hkv) >= (1ll << 30)) return AA_EUNSUPPORTED;
+    if (tokens >= (1 << 24)) return AA_EUNSUPPORTED;
     int rc = check_pool(p, p->kc, p->kc_stride, p->ks, p->ks_stride);
     if (rc == AA_OK) rc = check_pool(p, p->vc, p->vc_stride, p->vs, p->vs_stride);
     if (rc != AA_OK) return rc;
@@ -86,9 +83,9 @@ int make_args(const aa_kv_params* p, KvArgs* a) {
     return AA_OK;
 }
 
-KvSplit split_of(const aa_kv_params* p) {
+KvSplit split_of(const aa_kv_params* p, const KvArgs& a) {
     const long long room = (long long)p->max_pages * p->page_size;
-    return kv_split(p->B, p->Hq, p->Hkv, p->N, p->d, p->dtype, p->format, p->max_len && p->max_len < room ? p->max_len : room, room);
+    return kv_split(p->B, p->Hq, p->Hkv, p->N, a.total, p->d, p->dtype, p->format, p->max_len && p->max_len < room ? p->max_len : room, room);
 }
 
 int status_of(int rc, const char* name) {
@@ -123,7 +120,9 @@ int kv_attn_workspace_bytes(const aa_kv_params* params, size_t* bytes_out) {
     const int rc = make_args(params, &a);
     if (rc != AA_OK) return rc;
     if (!bytes_out) return AA_EINVAL;
-    *bytes_out = split_of(params).ws_bytes;
+    const KvSplit sp = split_of(params, a);
+    if (!sp.fits) return AA_EUNSUPPORTED;
+    *bytes_out = sp.ws_bytes;
     return AA_OK;
 }
 
@@ -133,7 +132,8 @@ int kv_attn(const aa_kv_params* params, const void* q, void* out, float* lse, vo
     if (rc != AA_OK) return rc;
     if (!q || !out || unaligned(q) || unaligned(out) || unaligned(ws)) return AA_EINVAL;
     if ((rc = check_rows(params, params->q_stride, a.Hq, false)) || (rc = check_rows(params, params->o_stride, a.Hq, true))) return rc;
-    const KvSplit sp = split_of(params);
+    const KvSplit sp = split_of(params, a);
+    if (!sp.fits) return AA_EUNSUPPORTED;
     if (sp.ws_bytes && !ws) return AA_EINVAL;
     if (ws_bytes < sp.ws_bytes) return AA_EWORKSPACE;
     return status_of(launch_kv_attn(a, params->dtype, params->format, params->d, sp, q, out, lse, (float*)ws, (hipStream_t)stream),

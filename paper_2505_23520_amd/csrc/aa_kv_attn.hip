@@ -624,8 +624,10 @@ __global__ __launch_bounds__(64 * kWaves, (kOccupancy<F, D, NT>)) void kv_attn_k
             }
         }
 
-        if (told && t == 0 && stop < s.units && threadIdx.x == 0) 
-            *told = Shared{s.b, hk, r0, (int)(deal_group(deal, at + s.units - 1) - blockIdx.x) + 1};
+        if (told && t == 0 && stop < s.units && threadIdx.x == 0) {
+            const int shares = (int)(deal_group(deal, at + s.units - 1) - blockIdx.x) + 1, left = p.groups - (int)blockIdx.x;
+            *told = Shared{s.b, hk, r0, shares < left ? shares : left};      // (more only if cu_seqlens does not ascend)
+        }
 
         // the next row tile
         at += stop - t;
@@ -805,11 +807,9 @@ int run(const AttnArgs& p, int R, hipStream_t st) {
     if (R == 16) return run_registers<F, D, 1>(p, st);
     if (R == 32) return run_registers<F, D, 2>(p, st);
     if constexpr (D < 128) return run_registers<F, D, 4>(p, st);
-    const long long x = (long long)p.a.Hkv * p.tiles * p.splits, join = p.splits == 1 ? 1 : (long long)p.a.Hkv * ((p.rows + 3) / 4);
-    if (x >= kMaxGrid || join >= kMaxGrid) return -1;
-    const int e = launch_kv_chunk(p, F == kRows4, dim3((unsigned)x, p.a.B), st);
+    const int e = launch_kv_chunk(p, F == kRows4, dim3((unsigned)(p.a.Hkv * p.tiles * p.splits), p.a.B), st);
     if (e != (int)hipSuccess || p.splits == 1) return e;
-    return (int)launch_kernel(kv_join_rows_kernel<T, D>, dim3((unsigned)join, p.a.B), dim3(256), 0, st, p);
+    return (int)launch_kernel(kv_join_rows_kernel<T, D>, dim3((unsigned)(p.a.Hkv * ((p.rows + 3) / 4)), p.a.B), dim3(256), 0, st, p);
 }
 
 template <int F, int D> int occupancy(int R) { return R == 16 ? kOccupancy<F, D, 1> : R == 32 ? kOccupancy<F, D, 2> : kOccupancy<F, D, 4>; }
@@ -818,11 +818,15 @@ constexpr int kCUs = 256;
 
 }  // namespace
 
-KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, long long longest, long long room) {
-    const long long rows = (long long)N * (Hq / Hkv), R = tile_rows(rows, d, dtype, format), tiles = (rows + R - 1) / R;
+KvSplit kv_split(int B, int Hq, int Hkv, int N, long long total, int d, int dtype, int format, long long longest, long long room) {
+    const long long grp = Hq / Hkv, rows = N * grp, R = tile_rows(rows, d, dtype, format), tiles = (rows + R - 1) / R;
     const long long items = tiles * B * Hkv;
-    KvSplit s = {0, 1, 0, 0};
+    KvSplit s = {0, 1, 0, 0, rows < (1ll << 30)};
     if (R < kChunkRows) {
+        // Units are counted in 32 bits, all rows' together: of a packed call the tiles that its rows can fill, not N for every sequence.
+        // Where that could be too many, a tile is one unit.
+        const long long line = Hkv * (total * grp / R + B < tiles * B ? total * grp / R + B : tiles * B);
+        s.fits = s.fits && line < (1ll << 31);
         // as many work-groups as run at once, or as there are units
         const int o = dtype == 0 ? (d == 32 ? occupancy<kRows32, 32>(R) : d == 64 ? occupancy<kRows32, 64>(R) : occupancy<kRows32, 128>(R))
                     : format ? (d == 64 ? occupancy<kRows4, 64>(R) : occupancy<kRows4, 128>(R))
@@ -832,7 +836,7 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
         // bf16, shared / whole, us: 1 x 512 keys 9.4 / 9.1, 1 x 1000 9.6 / 13.4, 8 x 1000 15.9 / 14.6, 16 x 2000 28.2 / 24.7,
         // 32 x 100 .. 1991 31.7 / 29.6, 64 x 512 26.3 / 24.1.
         const int tile_units = deal_units((int)longest, 1);
-        s.whole = tile_units <= 4 || (tile_units <= 16 && items >= 8 * tile_units);
+        s.whole = tile_units <= 4 || (tile_units <= 16 && items >= 8 * tile_units) || line * deal_units((int)room, 1) >= (1ll << 31);
         const long long units = items * (s.whole ? 1 : tile_units);
         s.groups = (int)(units < kCUs * o ? units : kCUs * o);
         if (!s.whole && room > kUnitKeys) s.ws_bytes = 2ull * s.groups * R * (d + 2) * 4 + s.groups * sizeof(Shared);
@@ -852,6 +856,8 @@ KvSplit kv_split(int B, int Hq, int Hkv, int N, int d, int dtype, int format, lo
     for (long long n = splits, most = 2 * splits + 2; n <= most && n * 512 <= longest; ++n)
         if (cost(n) < cost(splits)) splits = n;
     if (splits > kMaxShares) splits = kMaxShares;
+    if (Hkv * tiles * splits >= kMaxGrid || Hkv * ((rows + 3) / 4) >= kMaxGrid) splits = 1;
+    s.fits = s.fits && Hkv * tiles < kMaxGrid;
     s.splits = (int)splits;
     if (s.splits > 1) s.ws_bytes = (size_t)B * Hkv * rows * s.splits * (d + 2) * 4;
     return s;

@@ -661,3 +661,64 @@ def test_two_streams_and_repeats(api, dtype, fp4, n):
         torch.cuda.synchronize()
         for a, b in zip(want, outs):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ------------------------------------------------------------------ calls of the largest descriptions
+@pytest.mark.parametrize("dtype,fp4,d", [(BF, False, 128), (BF, True, 128), (BF, False, 64), (F32, False, 64)])
+def test_long_table_many_sequences(api, dtype, fp4, d):
+    """A packed step whose description allows far more than is there: 128 sequences of up to 8192 new tokens over a table of 131072."""
+    Hq, Hkv, page, N = 32, 8, 16, 8192
+    new = [i % 3 for i in range(127)] + [150]
+    lens = [n + (i * 37) % 300 for i, n in enumerate(new)]
+    T = sum(new)
+    cache = Cache(api, lens, Hkv, d, dtype, fp4, page, seed=5, room=131072 // page).fill()
+    x = _randn(N + 100, Hq + 2 * Hkv, d, seed=5, dtype=dtype).transpose(0, 1)
+    q, k, v = x.split([Hq, Hkv, Hkv])
+    ends = torch.tensor([0] + new).cumsum(0)
+    cu = ends.int().cuda()
+    qo, ko, _ = _append(api, cache, q, k, v, 0, cu=cu, max_new=N)
+    assert torch.equal(qo[:, :T], q[:, :T]) and torch.all(qo[:, T:] == 7.0)
+    back_k, back_v = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    api.kv_read(api.make_kv_params(cache.c, cache.table, cache.kv_len, k=back_k, v=back_v, cu_seqlens=cu, max_new=N), back_k, back_v)
+    out, lse = _attn(api, cache, q, cu, N)
+    for b, n in enumerate(new):
+        sl = slice(int(ends[b]), int(ends[b + 1]))
+        if n == 0:
+            continue
+        for got, src, key in ((back_k, k, "k"), (back_v, v, "v")):
+            want = fp4_values(*fp4_pack(src[:, sl])).cuda() if fp4 else src[:, sl].double()
+            assert torch.equal(got[:, sl].double(), want) and torch.equal(cache.rows(key, b, lens[b] - n, n), want)
+        want, wl, A, size = attend(q[:, sl].double(), cache.rows("k", b, 0, lens[b]), cache.rows("v", b, 0, lens[b]), lens[b] - n, 1 / math.sqrt(d))
+        to, tl = tolerances(want, A, size, wl, lens[b], d, dtype)
+        assert bool(((out[:, sl].double() - want).abs() <= to).all()) and bool(((lse[:, sl].double() - wl).abs() <= tl).all()), b
+    assert torch.all(back_k[:, T:] == 7.0) and torch.all(out[:, T:] == 7.0) and torch.all(lse[:, T:] == 7.0)
+
+
+@pytest.mark.parametrize("dtype,d", [(F32, 32), (BF, 64)])
+def test_units_beyond_32_bits(api, dtype, d):
+    """A table of 2^30 tokens and 256 tiles of rows: keys in units of 128 would be 2^31, so every tile is taken whole."""
+    n, length = 4096, 5000
+    cache = Cache(api, [length], 1, d, dtype, False, 1 << 20, seed=1, room=1024, spare=0).fill()
+    q = _randn(1, 4, n, d, seed=1, dtype=dtype)
+    p = api.make_kv_params(cache.c, cache.table, cache.kv_len, q=q, out=q)
+    assert api.kv_attn_workspace_bytes(p) == 0
+    _check_attn(api, cache, q, [n])
+
+
+@pytest.mark.parametrize("dtype,fp4,d", FORMATS)
+def test_rows_beyond_the_most(api, dtype, fp4, d):
+    """Of a packed sequence with more rows than max_new the first max_new take part, as its last tokens; the others stay as they were."""
+    new, lens, most = [5, 70, 3], [50, 300, 3], 40
+    cache = Cache(api, lens, 2, d, dtype, fp4, 16, seed=1).fill()
+    q = _randn(8, 78, d, seed=1, dtype=dtype)
+    cu = torch.tensor([0, 5, 75, 78], dtype=torch.int32, device="cuda")
+    out, lse = _attn(api, cache, q, cu, most)
+    at = 0
+    for b, n in enumerate(new):
+        m = min(n, most)
+        sl = slice(at, at + m)
+        want, wl, A, size = attend(q[:, sl].double(), cache.rows("k", b, 0, lens[b]), cache.rows("v", b, 0, lens[b]), lens[b] - m, 1 / math.sqrt(d))
+        to, tl = tolerances(want, A, size, wl, lens[b], d, dtype)
+        assert bool(((out[:, sl].double() - want).abs() <= to).all()) and bool(((lse[:, sl].double() - wl).abs() <= tl).all()), b
+        assert torch.all(out[:, at + m:at + n] == 7.0) and torch.all(lse[:, at + m:at + n] == 7.0)
+        at += n

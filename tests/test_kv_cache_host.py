@@ -301,3 +301,38 @@ def test_matrix_results_are_waited_for(compiled):
             kernels += any(t.startswith("v_mfma") for _, b in blocks for t in b)
             assert not _too_early(blocks), name
     assert kernels == 20
+
+
+def _accepted(api, p):
+    """What the workspace query, kv_append, kv_read and kv_attn say to the description alone: each call has a fault that is looked for after it."""
+    n, ref = ctypes.c_size_t(), ctypes.byref(p)
+    return (api._lib.kv_attn_workspace_bytes(ref, ctypes.byref(n)), api._lib.kv_append(ref, 4096, None, None, 4096, None, None, None, None),
+            api._lib.kv_read(ref, None, None, None), api._lib.kv_attn(ref, None, 4096, None, 4096, 1 << 40, None))
+
+
+@pytest.mark.parametrize("form", [dict(), dict(format=1), dict(d=64, rot_dim=64), dict(d=64, rot_dim=64, format=1), dict(dtype=0), dict(dtype=0, d=32, rot_dim=32)])
+@pytest.mark.parametrize("B,N,rows,room", [(1, 131072, 131072, 1 << 20), (1, 131072, 131072, 1 << 30), (16, 131072, 131200, 131072), (64, 16384, 20000, 131072),
+                                           (128, 8192, 9000, 131072), (256, 4096, 5000, 131072), (64, 1 << 20, 1 << 20, 131072), (4000, 1, 4000, 1 << 30),
+                                           (64, 100000, (1 << 24) - 1, 1 << 20)])
+def test_large_batches_are_taken(api, form, B, N, rows, room):
+    """Packed batches with a long table and one long prompt among the sequences, 32 / 8 heads: no entry point has a reason to refuse them."""
+    p = _params(api, B=B, N=N, Hq=32, Hkv=8, cu_seqlens=4096, total_tokens=rows, page_size=1024, max_pages=room >> 10, table_stride=room >> 10, **form)
+    for f in ("kc_stride", "vc_stride"):
+        setattr(p, f, _three(8 * 1024 * 128, 1024 * 128, 128))
+    for f in ("ks_stride", "vs_stride"):
+        setattr(p, f, _three(8 * 4 * 1024, 4 * 1024, 1024))
+    assert _accepted(api, p) == (api.AA_OK, api.AA_EINVAL, api.AA_EINVAL, api.AA_EINVAL)
+    p.cu_seqlens, p.N = None, max(1, ((1 << 24) - 1) // B)            # as many rows in a batch as a call may have
+    assert _accepted(api, p) == (api.AA_OK, api.AA_EINVAL, api.AA_EINVAL, api.AA_EINVAL)
+
+
+@pytest.mark.parametrize("kw", [dict(B=65535, Hq=65535, Hkv=65535), dict(Hq=65535, Hkv=1, N=(1 << 24) - 1), dict(Hq=65535, Hkv=65535, N=(1 << 24) - 1),
+                                dict(Hq=65535, Hkv=65535, N=(1 << 24) - 1, d=64, rot_dim=0)])
+def test_attention_that_cannot_be_counted(api, kw):
+    """Tiles of rows beyond 32 bits: refused by the workspace query and by kv_attn, alike; kv_append and kv_read have no tiles."""
+    p = _params(api, **dict(dict(B=1), **kw))
+    n, ref = ctypes.c_size_t(), ctypes.byref(p)
+    assert _accepted(api, p)[:3] == (api.AA_EUNSUPPORTED, api.AA_EINVAL, api.AA_EINVAL)
+    for f in ("q_stride", "o_stride"):
+        setattr(p, f, _three(1 << 39, 128, 1 << 23))
+    assert api._lib.kv_attn(ref, 4096, 4096, None, 4096, 1 << 40, None) == api.AA_EUNSUPPORTED
