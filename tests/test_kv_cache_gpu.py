@@ -273,6 +273,33 @@ def test_attn_values_not_finite(api, dtype, fp4, d, n):
             assert torch.equal(got.nan_to_num(nan=5.0), extra[~fine].nan_to_num(nan=5.0)), (b, i)
 
 
+@pytest.mark.parametrize("dtype,fp4,d", FORMATS)
+@pytest.mark.parametrize("Hq,length", [(8, 2500), (8, 400), (64, 9000)])
+def test_attn_nan_in_one_share(api, dtype, fp4, d, Hq, length):
+    """A NaN key, and a NaN value, far from the end of keys that several work-groups take: rows that see it are NaN (values: in their
+    channels), with a NaN lse for the key; the rows before it and the other KV head's are right."""
+    n, at = 150, length - 100                              # new tokens 50 .. see it
+    q = _randn(1, Hq, n, d, seed=3, dtype=dtype)
+    for key in ("k", "v"):
+        cache = Cache(api, [length], 2, d, dtype, fp4, 64, seed=3).fill()
+        K, V = cache.rows("k", 0, 0, length), cache.rows("v", 0, 0, length)
+        page, row = cache._at(0, at, 1)
+        if fp4:
+            cache.c[key + "_scale"][page, 0, 1, row] = 255
+        else:
+            cache.c[key][page, 0, row, 40 % d] = math.nan
+        out, lse = _attn(api, cache, q)
+        want, wl, A, size = attend(q[0].double(), K, V, length - n, 1 / math.sqrt(d))
+        to, tl = tolerances(want, A, size, wl, length, d, dtype)
+        bad = torch.zeros(Hq, n, d, dtype=torch.bool, device="cuda")
+        bad[:Hq // 2, 50:, slice(None) if key == "k" else slice(32, 64) if fp4 else 40 % d] = True
+        assert torch.equal(torch.isnan(out[0]), bad)
+        assert torch.equal(torch.isnan(lse[0]), bad.all(dim=2))
+        fine = ~bad
+        assert bool(((out[0].double() - want).abs()[fine] <= to[fine]).all())
+        assert bool(((lse[0].double() - wl).abs() <= tl)[~bad.all(dim=2)].all())
+
+
 @pytest.mark.parametrize("fp4", [False, True])
 def test_offsets_beyond_32_bits(api, fp4):
     """A pool whose last pages lie beyond 2^32 bytes: appended to, read and attended there."""

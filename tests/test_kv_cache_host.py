@@ -190,6 +190,14 @@ int main() {
     assert run.returncode == 0
 
 
+def test_cache_kernels_honour_nans():
+    """A NaN among a row's keys or values has to reach its result and lse: no source of the cache is compiled as if there were none."""
+    from paper_2505_23520_amd import build
+    relaxed = {"-fno-honor-nans", "-fno-honor-infinities", "-ffinite-math-only", "-ffast-math", "-Ofast"}
+    for source in build.CACHE_SOURCES:
+        assert not relaxed & set(build.FLAGS + build.EXTRA.get(source, [])), source
+
+
 @pytest.fixture(scope="module")
 def compiled(tmp_path_factory):
     """The cache's kernel sources compiled as the build does: source -> (the compiler's report on registers, assembly)."""
