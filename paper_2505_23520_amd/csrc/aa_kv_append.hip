@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "aa_kv.h"
+#include "aa_kv_turn.h"
 
 namespace aa {
 namespace {
@@ -32,20 +33,6 @@ template <class T> __device__ __forceinline__ u32x4 pack(const float* x) {
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) v.t[i] = (T)x[i];
     return v.u;
-}
-
-// Cosine and sine of x, |x| <= pi / 4, by their series: the first term left out is below 2^-24 (float) or 2^-54 (double) of the result.
-__device__ __forceinline__ void series(float x, float* c, float* s) {
-    const float y = x * x;
-    *c = 1.f + y * (-1.f / 2 + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320 + y * (-1.f / 3628800)))));
-    *s = x + x * y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880))));
-}
-__device__ __forceinline__ void series(double x, double* c, double* s) {
-    const double y = x * x;
-    *c = 1. + y * (-1. / 2 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 + y * (-1. / 3628800 +
-              y * (1. / 479001600 + y * (-1. / 87178291200. + y * (1. / 20922789888000.))))))));
-    *s = x + x * y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880 + y * (-1. / 39916800 +
-              y * (1. / 6227020800. + y * (-1. / 1307674368000.)))))));
 }
 
 // Cosine and sine of the angle t.  The angle and what is left of it after whole quarter turns are 64-bit numbers (a position of a million

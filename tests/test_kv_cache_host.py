@@ -145,6 +145,33 @@ int main() {
     assert [int(t) for t in got] == scales[:, 0].tolist()
 
 
+def test_series_on_the_host(tmp_path):
+    """The sine and cosine series evaluated in 64 bits of mantissa: what they leave out stays within their bounds (and 2^-60 for the evaluation's
+    own roundings) up to pi / 4."""
+    src, exe = tmp_path / "s.cpp", str(tmp_path / "s")
+    src.write_text('''#include "%s/paper_2505_23520_amd/csrc/aa_kv_turn.h"
+#include <cmath>
+#include <stdio.h>
+int main() {
+    static_assert(__LDBL_MANT_DIG__ >= 64, "");
+    long double worst[2] = {0, 0};
+    for (int i = -20000; i <= 20000; ++i) {
+        const long double x = i / 20000.0L * 0.78539816339744830962L;
+        long double c, s;
+        for (int k = 0; k < 2; ++k) {
+            if (k) aa::series64(x, &c, &s); else aa::series32(x, &c, &s);
+            const long double ec = fabsl(c - cosl(x)) / cosl(x), es = i ? fabsl(s - sinl(x)) / fabsl(sinl(x)) : fabsl(s);
+            if (ec > worst[k]) worst[k] = ec;
+            if (es > worst[k]) worst[k] = es;
+        }
+    }
+    printf("%%La %%La\\n", worst[0], worst[1]);
+    return worst[0] > 0x1p-24L + 0x1p-60L ? 1 : worst[1] > 0x1p-54L + 0x1p-60L ? 2 : 0;
+}''' % ROOT)
+    subprocess.check_call(["g++", "-O1", "-std=c++17", str(src), "-o", exe])
+    assert subprocess.run([exe]).returncode == 0
+
+
 def test_deal_on_the_host(tmp_path):
     """Every unit belongs to exactly one work-group, the work-groups' numbers of units differ by one at most, and the places of the
     shares of a tile are all different, whatever the lengths."""
