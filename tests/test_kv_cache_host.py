@@ -258,6 +258,16 @@ def test_cache_kernels_do_not_spill(compiled):
             assert o >= waves(name), (name, o)
 
 
+def test_append_and_read_kernels_do_not_spill(compiled):
+    """One kernel of kv_append keeps up to 6 registers in scratch memory, by measurement: 4 bits, d = 128, halves, four tokens, three rows in flight."""
+    import re
+    report = compiled["aa_kv_append.hip"][0]
+    names, spills = re.findall(r"Function Name: (\S+)", report), [int(x) for x in re.findall(r"VGPRs Spill: (\d+)", report)]
+    assert len(names) == len(spills) and sum("kv_read_kernel" in n for n in names) == 7 and sum("kv_append_kernel" in n for n in names) == 63
+    for name, n in zip(names, spills):
+        assert n <= (6 if "kv_append_kernelIDF16bLb1ELi128ELi1ELi4ELi3E" in name else 0), (name, n)
+
+
 # Wait states between a matrix instruction and another instruction that reads or overwrites its result: two (products of floats) or three more
 # than its passes.
 WAIT_STATES = {"v_mfma_f32_16x16x4_f32": 10, "v_mfma_f32_16x16x32_bf16": 7, "v_mfma_f32_32x32x16_bf16": 11}
