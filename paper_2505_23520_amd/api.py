@@ -327,7 +327,7 @@ def make_kv_params(cache: dict, page_table, kv_len, q=None, k=None, v=None, out=
     if packed:
         ints.append(("cu_seqlens", cu_seqlens, (p.B + 1,)))
     for name, t, shape in ints:
-        if t.dtype != torch.int32 or tuple(t.shape) != shape or t.stride(-1) != 1:
+        if t.dtype != torch.int32 or tuple(t.shape) != shape or (t.shape[-1] > 1 and t.stride(-1) != 1):
             raise ValueError("%s: shape %s %s, expected contiguous int32 %s" % (name, tuple(t.shape), t.dtype, shape))
     held = list(given.values()) + [t for t in cache.values() if t is not None] + [page_table, kv_len] + ([cu_seqlens] if packed else [])
     if any(t.device != first.device for t in held):

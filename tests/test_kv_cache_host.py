@@ -125,6 +125,21 @@ def test_binding_rejects(api):
             api.kv_append(p, *args)
 
 
+def test_binding_takes_one_entry_of_any_stride(api):
+    """A batch of one whose length, row ends or only page are a column of another array: the stride of one entry is never used."""
+    c = api.alloc_kv_cache(6, 2, 16, 128, device="cpu")
+    q = torch.zeros(1, 8, 1, 128, dtype=torch.bfloat16)
+    many = torch.arange(12, dtype=torch.int32).view(4, 3)
+    lens, table = many.t()[:1, 2], many.t()[1:2, :1]
+    lens = torch.as_strided(lens, (1,), (3,), lens.storage_offset())
+    assert table.stride(-1) != 1 and lens.stride(0) != 1
+    p = api.make_kv_params(c, table, lens, q=q, out=q)
+    assert (p.B, p.max_pages, p.table_stride, p.kv_len) == (1, 1, 1, lens.data_ptr()) and p.page_table == table.data_ptr()
+    for t, n in ((many.t()[:1, :3], lens), (table, many[:2, 0])):
+        with pytest.raises(ValueError):
+            api.make_kv_params(c, t, n, q=q, out=q)
+
+
 def test_fp4_scale_on_the_host(tmp_path):
     """fp4_scale_byte against every exponent tried out."""
     from kv_util import fp4_pack
