@@ -348,7 +348,7 @@ def make_kv_params(cache: dict, page_table, kv_len, q=None, k=None, v=None, out=
     p.device = first.device
     p.new_rows = axis if packed else p.B * axis
     p.made_for = {name: (t.shape, t.stride(), t.dtype, t.device) for name, t in given.items()}
-    p.held, p.ref = held, ctypes.byref(p)
+    p.held = held
     return p
 
 
@@ -376,10 +376,10 @@ def _kv_call(fn, p, stream, *args):
     if at is None:
         raise ValueError("the tensors are on %s: the kernels need a GPU" % p.device)
     if torch.cuda.current_device() == at:
-        rc = fn(p.ref, *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+        rc = fn(ctypes.byref(p), *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(at):
-            rc = fn(p.ref, *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
+            rc = fn(ctypes.byref(p), *args, torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream)
     if rc != AA_OK:
         raise AnchorError(rc)
 

@@ -125,6 +125,21 @@ def test_binding_rejects(api):
             api.kv_append(p, *args)
 
 
+def test_params_let_their_tensors_go(api):
+    """A description keeps its tensors as long as it lives, and no longer: a server makes one for every packed step."""
+    import weakref
+    c = api.alloc_kv_cache(6, 2, 16, 128, device="cpu")
+    q, lens = torch.zeros(1, 8, 1, 128, dtype=torch.bfloat16), torch.ones(1, dtype=torch.int32)
+    p = api.make_kv_params(c, torch.zeros(1, 2, dtype=torch.int32), lens, q=q, out=q)
+    with pytest.raises(ValueError):
+        api.kv_attn(p, q, q)                             # (no GPU tensors)
+    seen = [weakref.ref(x) for x in (q, lens, p)]
+    del q, lens
+    assert all(r() is not None for r in seen)
+    del p
+    assert all(r() is None for r in seen)
+
+
 def test_binding_takes_one_entry_of_any_stride(api):
     """A batch of one whose length, row ends or only page are a column of another array: the stride of one entry is never used."""
     c = api.alloc_kv_cache(6, 2, 16, 128, device="cpu")
