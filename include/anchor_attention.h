@@ -304,6 +304,10 @@ int kv_attn_workspace_bytes(const aa_kv_params *params, size_t *bytes_out);
  * (lse nullable, laid out as the per-row arrays at the top).  A row that sees no key: out 0, lse -infinity.  Storage that a row
  * does not see (later tokens, behind the end, other pages) never reaches it, whatever its bits.  out and q must not overlap, and a
  * call has its workspace for itself until it is through.
+ * Sums are held in 32 bits.  bf16 calls round the softmax weights to bf16 (2^-8 of each at most) for their product with the values, not in
+ * their sum, and the result once; fp32 calls round nothing on the way.
+ * One way of working is chosen for all sequences of a call, by N*Hq/Hkv: where one sequence has many new tokens and many have one, two
+ * calls are faster.
  * Equal calls give equal bits.  The order of a row's sums depends on how the call's keys are dealt out, and so on the lengths of its
  * other sequences and on max_len.
  */

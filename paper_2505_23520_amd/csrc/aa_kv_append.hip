@@ -6,8 +6,8 @@
 // element.  A work-group takes a token, or four (see run_pairs): a wave for each works out where it lies and the cosines and sines of its
 // position, one angle a lane, for all heads; then the threads take 16 bytes of a row each, a pair's other half being read a
 // second time from the L1, and the rows of a token that one thread meets are in flight together.
-// 51393 tokens of 32 / 8 heads, d = 128, bf16: 1.37 GB in 263 us, 5.2 TB/s (a copy of 4 GB: 4.7).  16384 tokens into 4 bits: 0.39 GB in
-// 97 us, 4.0 TB/s, the 64-bit turning of the keys standing beside the traffic; kv_read of them 85 MB in 21 us, 4.0 TB/s.  One token: 3.4 us,
+// 51393 tokens of 32 / 8 heads, d = 128, bf16: 1.37 GB in 260 us, 5.3 TB/s (a copy of 4 GB: 4.7).  16384 tokens into 4 bits: 0.39 GB in
+// 97 us, 4.0 TB/s, the 64-bit turning of the keys standing beside the traffic; kv_read of them 85 MB in 21 us, 4.0 TB/s.  One token: 3.3 us,
 // which is a launch and four dependent reads (length, page, then the row).
 #include <type_traits>
 
@@ -322,10 +322,10 @@ int run_pairs(const AppendArgs& p, hipStream_t st) {
     constexpr int ROWS = 256 / (D / kVec<T>);                      // rows of a token that a work-group takes at once
     const int rows = (p.q_out ? p.a.Hq : 0) + (p.k ? 2 * p.a.Hkv : 0);
     // A work-group a token, or four of them: what is worked out once a work-group is shared by more, but a token waits for the one before.
-    // A token / four, us, d = 128, tokens 300, 2000, 8000, 51000; plain pages, 48 rows (32 / 8 heads) 5.2 / 8.4, 12.3 / 13.4, 44.3 / 48.2,
-    // 253 / 266; 24 rows (8 / 8) 4.6 / 7.2, 9.7 / 10.6, 23.5 / 22.5, 164 / 146; 8 rows (4 / 2) 4.3 / 5.9, 7.7 / 7.5, 21.5 / 16.4, 126 / 81;
-    // 4 bits, where the angles take 64 bits to the end, 48 rows 11.1 / 15.4, 23.4 / 21.9, 66 / 64, 371 / 351; 8 rows 9.8 / 12.1, 15.4 / 13.5,
-    // 42 / 26, 231 / 128.
+    // A token / four, us, d = 128, tokens 300, 2000, 8000, 51000, the same rows again and again: plain pages, 48 rows (32 / 8 heads) 4.6 / 7.9,
+    // 10.7 / 11.9, 31.7 / 32.6, 217 / 229; 24 rows (8 / 8) 4.0 / 6.8, 8.5 / 9.4, 22.3 / 20.4, 152 / 133; 8 rows (4 / 2) 3.7 / 5.6, 7.2 / 7.0,
+    // 20.1 / 14.3, 106 / 61; 4 bits, where the angles take 64 bits to the end, 48 rows 6.7 / 11.0, 16.0 / 15.5, 47.7 / 37.4, 307 / 251; 8 rows
+    // 5.7 / 8.1, 11.3 / 9.2, 35.7 / 19.0, 204 / 87.
     if (p.a.total < (FP4 || rows <= ROWS ? 2000 : 4000) || (!FP4 && rows > 2 * ROWS)) {
         const int passes = (rows + 3 * ROWS - 1) / (3 * ROWS);
         return (int)launch_kernel(kv_append_kernel<T, FP4, D, PAIRS, 1, 3>, dim3((unsigned)p.a.total, passes < 64 ? passes : 64), dim3(256), 0, st, p);

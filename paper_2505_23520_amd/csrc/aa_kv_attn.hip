@@ -17,8 +17,8 @@
 // Roundings to bf16: the weights (2^-8 each at most, as the matrix instruction takes them; their sum l is of the unrounded ones) and the
 // result.  Codes of 4 bits are bf16 numbers exactly.  Float caches stay 32 bits throughout.
 // Bound by memory for few rows: one token over 131072 keys of 8 heads, d = 128, bf16 537 MB in 92 us, 5.8 TB/s (a pure read of 4 GB by the
-// library's sum: 4.0); 32 sequences of 200 .. 16000 in 134 us, 5.6; 64 sequences in 4 bits 552 MB in 112 us, 5.0, where the conversion of the
-// codes takes a third of the vector unit's time beside it.  1000 keys: 6.3 us and the join 3, both latency.
+// library's sum: 4.0); 32 sequences of 200 .. 16000 in 134 us, 5.6; 64 sequences in 4 bits 552 MB in 109 us, 5.1, where the conversion of the
+// codes takes a third of the vector unit's time beside it.  1000 keys: 6.4 us and the join 3, both latency.
 #include "aa_kv_attn.h"
 
 namespace aa {

@@ -12,8 +12,8 @@
 // Rows of values behind the last key, or without storage, are cleared in LDS: their weight is 0, their bits may be anything.  What is not
 // finite in a tile that some row does not see whole is added to the rows that see it, and cleared before the product.
 // Bound by the matrix pipe and a wave's own chain, as that engine: 2048 and 1000 new tokens over 30011 and 8192, 32 / 8 heads, bf16 1.10 TFLOP
-// in 1000 us, 1.1 PFLOP/s (a large matrix product: 1.26); 1024 and 403 over 16384 and 5003 in 4 bits 0.30 TFLOP in 345 us and the join 20
-// (6144 over 16384, three work-groups a CU and no join: 1.04).
+// in 986 to 1058 us by card, 1.04 to 1.11 PFLOP/s (a large matrix product: 1.26); 1024 and 403 over 16384 and 5003 in 4 bits 0.30 TFLOP in 354
+// to 371 us with the join (6144 over 16384, three work-groups a CU and no join: 1.04).
 #include "aa_engine_bf16_common.h"
 #include "aa_kv_attn.h"
 
