@@ -46,15 +46,20 @@ MFMA_BF16_PEAK = 2.5e15   # MI355X dense bf16, FLOP/s
 HBM_PEAK = 8.0e12         # B/s
 
 
+def kernel_sources():
+    """Names of the sources that the prefill's kernels are built from: all but the paged cache's, which nothing here calls."""
+    csrc = os.path.join(ROOT, "paper_2505_23520_amd", "csrc")
+    return [name for name in sorted(os.listdir(csrc)) if name.endswith((".hip", ".h")) and not name.startswith("aa_kv")]
+
+
 def kernel_sources_sha256():
-    """Digest of the kernel sources of this tree: counter summaries under profiles/ carry the digest
+    """Digest of the prefill's kernel sources of this tree: counter summaries under profiles/ carry the digest
     of the build they were measured on, and are quoted only when it is this one."""
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2505_23520_amd", "csrc")
-    for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".h")):
-            h.update(name.encode())
-            h.update(open(os.path.join(csrc, name), "rb").read())
+    for name in kernel_sources():
+        h.update(name.encode())
+        h.update(open(os.path.join(csrc, name), "rb").read())
     return h.hexdigest()[:16]
 
 

@@ -219,3 +219,17 @@ def test_null_pointers_and_workspace_are_rejected_on_host(api):
     assert lib.anchor_attention_prefill(ctypes.byref(p), P(4097), fake, fake, fake, None, None, fake, 16, None) \
         == api.AA_EINVAL
     assert api._lib.anchor_strerror(-3) == b"workspace too small"
+
+
+def test_bench_digest_covers_the_prefill_alone():
+    """bench.py quotes counter summaries of builds with the same kernel sources: all that the prefill's sources include, and none of the paged cache's,
+    which the benchmark never calls."""
+    import bench
+    from paper_2505_23520_amd import build
+    need, todo = set(), list(build.SOURCES)
+    while todo:
+        name = todo.pop()
+        if name not in need:
+            need.add(name)
+            todo += re.findall(r'#include "([^"/]+)"', open(os.path.join(build.CSRC, name)).read())
+    assert set(bench.kernel_sources()) == need and not need & set(build.CACHE_SOURCES)
